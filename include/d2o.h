@@ -287,6 +287,96 @@ d2o_status d2o_layer_stats_static(int32_t dtype, int32_t d_head, int32_t batch, 
                                   int32_t n_kv_heads, int32_t prompt_len, const void* Q, const void* K,
                                   float* colsum, double* density, void* stream);
 
+/* Attention of a prompt (Section 3, Eq. 2-3, over all positions at once): what a model computes before d2o_layer_stats and
+ * d2o_prefill_compress take its keys and values, with a causal mask and, where a model limits its view (the sliding-window
+ * caches with sink tokens of the related work, Section 2), a window:
+ *
+ *   out_i = sum_j p_ij v_j,  p_ij = exp(q_i.k_j / sqrt(d) - lse_i),  lse_i = ln sum_j exp(q_i.k_j / sqrt(d)),
+ *   j over the positions that i sees: j <= i, and with window > 0 only j > i - window or j < n_sink.
+ *
+ * Q and out DEVICE [B, Hq, P, d], K and V DEVICE [B, Hkv, P, d] in `dtype`; lse DEVICE float [B, Hq, P], natural log (what
+ * d2o_layer_stats takes where window is 0), may be NULL; lens DEVICE int32 [B], the length of every sequence (0 ..
+ * prompt_len), may be NULL: all prompt_len.  Rows of Q, K and V at and behind a sequence's length are padding: they may hold
+ * anything, and those of out and lse stay as they were.  A length outside 0 .. prompt_len counts as the nearer end.
+ * Inside a sequence a value that is not finite reaches the rows that see it, and may reach rows of the same 256 queries that do
+ * not (0 * inf).
+ * 16-bit inputs run on the tensor cores, the weights p rounded to the input type for their product with V (relative to the
+ * row's largest; sums and lse from the unrounded weights); fp32 inputs on CUDA cores, in fp32 throughout.
+ * status DEVICE uint32 [2], may be NULL: error word and detail (D2O_ERR_TIMEOUT: a device-side wait ran out; rows that were in
+ * hand are NaN).  No context, no scratch; asynchronous.
+ * Limits: B * Hq * P < 2^31; d_head 64 or 128; Hq / Hkv any whole number. */
+d2o_status d2o_prompt_attention(int32_t dtype, int32_t d_head, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                int32_t prompt_len, int32_t window, int32_t n_sink, const void* Q, const void* K,
+                                const void* V, const int32_t* lens, void* out, float* lse, uint32_t* status, void* stream);
+
+/* A key-value cache in pages, one layer of it: the cache of a serving program that hands out memory page by page.  Row r of
+ * KV head h of sequence b lies in page page_table[b, r / page_size] at [h, r % page_size].  The caller owns everything,
+ * page_table and len included, and changes them between the calls, on the stream; the library never writes them, so that the
+ * calls below can be captured into a graph and replayed while the sequences grow.
+ *
+ * Rows of a sequence may lie in pages that another sequence's table names too (a common prefix) as long as nothing is written
+ * there: the page that d2o_paged_decode_step or d2o_paged_append writes to, and with `score` every page of a sequence, belongs
+ * to one sequence and stands in its table once.  Otherwise the rows and scores written there are undefined.
+ *
+ * What a call reads on the device is checked there: a page number outside 0 .. n_pages - 1, or a length that the table does
+ * not reach, sets the error word and nothing is read or written through it (see each call). */
+typedef struct {
+  int32_t dtype;                 /* d2o_dtype of pages, inputs and outputs                                           */
+  int32_t d_head;                /* 64 or 128                                                                        */
+  int32_t batch;                 /* [B] sequences                                                                    */
+  int32_t n_q_heads, n_kv_heads; /* n_q_heads / n_kv_heads = 1, 2, 4 or 8                                            */
+  int32_t page_size;             /* rows per page and KV head: a power of two, 16 .. 1024                            */
+  int32_t n_pages;               /* pages of the pools; n_pages * n_kv_heads * page_size < 2^31                      */
+  int32_t max_pages;             /* entries per row of page_table                                                    */
+  void*    k_pages;              /* DEVICE [n_pages, Hkv, page_size, d]                                              */
+  void*    v_pages;              /* DEVICE [n_pages, Hkv, page_size, d]                                              */
+  int32_t* pos;                  /* DEVICE [n_pages, Hkv, page_size] original position of each row; NULL: not kept   */
+  float*   score;                /* DEVICE [n_pages, Hkv, page_size] accumulated attention score (Eq. 6); NULL: not kept.
+                                  * pos and score are both given or both NULL                                        */
+  const int32_t* page_table;     /* DEVICE [B, max_pages]                                                            */
+  const int32_t* len;            /* DEVICE [B, Hkv] rows held; negative: there is no such sequence (a padded batch),
+                                  * nothing of it is read or written                                                 */
+  uint32_t* status;              /* DEVICE [2] error word and detail, first anomaly stays; NULL: not reported        */
+} d2o_paged_cache;
+
+/* Bytes of DEVICE scratch (256-byte aligned) that d2o_paged_decode_step and d2o_paged_evict need for this cache (only the
+ * sizes and whether `score` is NULL count).  Contents need not be kept or cleared between calls; two calls whose work may
+ * overlap on the GPU need a scratch each, also as parts of graphs. */
+d2o_status d2o_paged_workspace_size(const d2o_paged_cache* cache, size_t* bytes);
+
+/* Puts the rows of a prompt, or of a turn, behind those held: row i of sequence b goes to row len[b, h] + i, for i < lens[b].
+ * K, V DEVICE [B, Hkv, n_rows, d]; lens DEVICE int32 [B] (0 .. n_rows; NULL: n_rows each).  With pos and score: row i gets
+ * position first_pos[b] + i (DEVICE int32 [B]; NULL: i) and, as score, the sum of colsum [B, Hq, n_rows] over the query heads of
+ * its KV head in their order (DEVICE float, the column sums of d2o_layer_stats: Eq. 6 case 1; NULL: 0).  first_pos and colsum
+ * without pos and score are D2O_ERR_INVALID_ARG.  Rows that the table does not reach, or whose page number is bad, are not
+ * written and set the error word.  The caller adds lens to len.  Asynchronous. */
+d2o_status d2o_paged_append(const d2o_paged_cache* cache, int32_t n_rows, const void* K, const void* V, const int32_t* lens,
+                            const int32_t* first_pos, const float* colsum, void* stream);
+
+/* One generated token per sequence (Eq. 2-3): (k, v) goes to row t = len[b, h], and the query heads of h attend over the rows
+ * r <= t, with window > 0 only r > t - window or r < n_sink.  Rows count in the order in which they lie in the pages: a cache
+ * that d2o_paged_evict has been through is no longer in the order of positions, so that a window has no meaning there.
+ * q, out DEVICE [B, Hq, d]; k, v DEVICE [B, Hkv, d].  With pos and score: row t gets positions[b] (DEVICE int32 [B]; NULL: t),
+ * its weight, summed over the query heads, as score, and every other row that is seen has its weight added to its score (Eq. 6
+ * case 2).  A sequence whose table does not reach row t, or has a bad page number among the rows seen, gets NaN outputs in the
+ * heads concerned and sets the error word.  Rows outside the view may hold anything.  The caller adds one to len.
+ * The rows of all sequences together are divided evenly over the GPU, whatever the single lengths, and what was divided is
+ * joined again in a fixed order: results do not change from run to run.  Asynchronous. */
+d2o_status d2o_paged_decode_step(const d2o_paged_cache* cache, int32_t window, int32_t n_sink, const void* q, const void* k,
+                                 const void* v, const int32_t* positions, void* out, void* scratch, size_t scratch_bytes,
+                                 void* stream);
+
+/* Eviction without merging (Eq. 7-8, tau = +inf): of the len[b, h] rows min(len, budgets[b, h]) stay (budgets DEVICE int32
+ * [B, Hkv], as d2o_budgets_from_density gives them), and lie in the first rows of the slice afterwards.  Rows whose position is
+ * below n_sink or at least next_pos[b] - window (next_pos DEVICE int32 [B]: tokens seen so far) stay ahead of all others, the
+ * others by score; ties by position, the earlier one stays; +0 and -0 are equal, a NaN counts as higher than every number.  Kept
+ * rows that lie below the budget stay where they are; those behind it move, in their order, into the rows below that are given
+ * up, in theirs.  Rows behind the budget keep their contents.  The caller sets len to min(len, budgets).  Needs pos and score.
+ * A slice whose table does not reach its rows, or has a bad page number among them, or a negative budget, is left as it was and
+ * sets the error word.  Asynchronous. */
+d2o_status d2o_paged_evict(const d2o_paged_cache* cache, const int32_t* budgets, const int32_t* next_pos, int32_t n_sink,
+                           int32_t window, void* scratch, size_t scratch_bytes, void* stream);
+
 d2o_status d2o_get_view(d2o_ctx* ctx, int32_t layer, d2o_view* out);
 /* Copies the counters to HOST memory; synchronises `stream`. */
 d2o_status d2o_get_stats(d2o_ctx* ctx, d2o_stats* out_host, void* stream);

@@ -26,6 +26,7 @@ EXPORTS = [
     "d2o_layer_stats", "d2o_layer_stats_layers", "d2o_layer_budgets", "d2o_budgets_from_density", "d2o_prefill_compress",
     "d2o_prefill_compress_layers", "d2o_decode_step", "d2o_decode_steps", "d2o_decode_step_host", "d2o_decode_steps_host", "d2o_full_decode_step", "d2o_get_view", "d2o_get_stats",
     "d2o_set_tuning", "d2o_layer_stats_static", "d2o_set_fault_injection", "d2o_set_prompt_lens",
+    "d2o_prompt_attention", "d2o_paged_workspace_size", "d2o_paged_append", "d2o_paged_decode_step", "d2o_paged_evict",
 ]
 STATIC_LSE_FLOATS = 1 << 20      # D2O_STATIC_LSE_FLOATS of include/d2o.h
 
@@ -53,6 +54,14 @@ class D2OStats(C.Structure):
                 ("discards", C.c_uint64), ("prefill_evicted", C.c_uint64), ("prefill_merged", C.c_uint64),
                 ("error_word", C.c_uint32), ("error_detail", C.c_uint32), ("decode_launches", C.c_uint64),
                 ("guess_misses", C.c_uint64)]
+
+
+class D2OPaged(C.Structure):
+    """d2o_paged_cache of include/d2o.h."""
+    _fields_ = [("dtype", C.c_int32), ("d_head", C.c_int32), ("batch", C.c_int32), ("n_q_heads", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("pos", C.c_void_p), ("score", C.c_void_p),
+                ("page_table", C.c_void_p), ("len", C.c_void_p), ("status", C.c_void_p)]
 
 
 class D2OError(RuntimeError):
@@ -105,6 +114,12 @@ def load_library() -> C.CDLL:
     lib.d2o_layer_stats_static.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
     lib.d2o_set_fault_injection.argtypes = [vp, i32, i32]
     lib.d2o_set_prompt_lens.argtypes = [vp, vp, vp]
+    pg = C.POINTER(D2OPaged)
+    lib.d2o_prompt_attention.argtypes = [i32] * 8 + [vp] * 8
+    lib.d2o_paged_workspace_size.argtypes = [pg, C.POINTER(C.c_size_t)]
+    lib.d2o_paged_append.argtypes = [pg, i32, vp, vp, vp, vp, vp, vp]
+    lib.d2o_paged_decode_step.argtypes = [pg, i32, i32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.d2o_paged_evict.argtypes = [pg, vp, vp, i32, i32, vp, C.c_size_t, vp]
     for name in EXPORTS:
         if name not in ("d2o_status_string", "d2o_last_cuda_error", "d2o_destroy"):
             getattr(lib, name).restype = C.c_int
@@ -376,3 +391,106 @@ def d2o_layer_stats_static(Q: torch.Tensor, K: torch.Tensor, colsum: torch.Tenso
     assert density.dtype == torch.float64 and tuple(density.shape) == (B, Hq)
     _check(lib.d2o_layer_stats_static(DTYPE_CODE[Q.dtype], d, B, Hq, Hkv, P, _ptr(Q), _ptr(K), _ptr(colsum),
                                       _ptr(density), _stream()), "d2o_layer_stats_static")
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise D2OError(1, what)
+
+
+def _arg(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> Optional[int]:
+    """The address of a tensor that has to be contiguous, of this shape and type and on this device (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise D2OError(1, f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, got "
+                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _call(device: torch.device, what: str, fn, *args):
+    """fn(*args, stream) with the tensors' device current: their stream is that device's current one."""
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream()), what)
+        return
+    with torch.cuda.device(device):
+        _check(fn(*args, _stream()), what)
+
+
+def d2o_prompt_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out: torch.Tensor, *,
+                         lse: Optional[torch.Tensor] = None, window: int = 0, n_sink: int = 0,
+                         lens: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None):
+    """Causal attention of a prompt, over a window and the first `n_sink` tokens where `window` > 0.
+
+    Q, out [B, Hq, P, d], K, V [B, Hkv, P, d]; lse float32 [B, Hq, P] (natural log: the `lse` of d2o_layer_stats where
+    there is no window); lens int32 [B], status int32 [2], all on the GPU."""
+    _need(Q.dim() == 4 and K.dim() == 4 and Q.dtype in DTYPE_CODE and Q.is_cuda, "Q, K: [B, H, P, d] on the GPU")
+    b, hq, n, d = Q.shape
+    hkv, dev = K.shape[1], Q.device
+    _call(dev, "d2o_prompt_attention", load_library().d2o_prompt_attention, DTYPE_CODE[Q.dtype], d, b, hq, hkv, n, window, n_sink,
+          _arg(Q, "Q", (b, hq, n, d), Q.dtype, dev), _arg(K, "K", (b, hkv, n, d), Q.dtype, dev),
+          _arg(V, "V", (b, hkv, n, d), Q.dtype, dev), _arg(lens, "lens", (b,), torch.int32, dev),
+          _arg(out, "out", (b, hq, n, d), Q.dtype, dev), _arg(lse, "lse", (b, hq, n), torch.float32, dev),
+          _arg(status, "status", (2,), torch.int32, dev))
+
+
+class D2OPagedCache:
+    """One layer of a key-value cache in pages (d2o_paged_cache of include/d2o.h): holds the caller's tensors and owns the
+    scratch and the error word; methods mirror the C entry points.
+
+    k_pages, v_pages [n_pages, Hkv, page_size, d]; page_table int32 [B, max_pages]; length int32 [B, Hkv], rows held
+    (negative: no such sequence); pos int32 and score float32 [n_pages, Hkv, page_size], both or neither.  The caller
+    changes the contents of page_table and length between the calls, in place; the library never does."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, length: torch.Tensor, *,
+                 n_q_heads: int, pos: Optional[torch.Tensor] = None, score: Optional[torch.Tensor] = None):
+        self.lib = load_library()
+        _need(k_pages.dim() == 4 and k_pages.dtype in DTYPE_CODE and k_pages.is_cuda, "k_pages: [n_pages, Hkv, page_size, d] on the GPU")
+        _need(page_table.dim() == 2, "page_table: [B, max_pages]")
+        n_pages, hkv, page, d = k_pages.shape
+        b, max_pages = page_table.shape
+        dev = self.device = k_pages.device
+        self.dtype, self.shape = k_pages.dtype, (b, n_q_heads, hkv, d)
+        self.status = torch.zeros(2, dtype=torch.int32, device=dev)
+        self.tensors = (k_pages, v_pages, page_table, length, pos, score)
+        self.cache = D2OPaged(
+            DTYPE_CODE[k_pages.dtype], d, b, n_q_heads, hkv, page, n_pages, max_pages,
+            _arg(k_pages, "k_pages", k_pages.shape, k_pages.dtype, dev), _arg(v_pages, "v_pages", k_pages.shape, k_pages.dtype, dev),
+            _arg(pos, "pos", (n_pages, hkv, page), torch.int32, dev), _arg(score, "score", (n_pages, hkv, page), torch.float32, dev),
+            _arg(page_table, "page_table", (b, max_pages), torch.int32, dev), _arg(length, "length", (b, hkv), torch.int32, dev),
+            self.status.data_ptr())
+        n = C.c_size_t()
+        _check(self.lib.d2o_paged_workspace_size(C.byref(self.cache), C.byref(n)), "d2o_paged_workspace_size")
+        self.scratch = torch.empty(n.value + 256, dtype=torch.uint8, device=dev)
+        self._scratch = ((self.scratch.data_ptr() + 255) // 256 * 256, n.value)
+
+    def d2o_paged_append(self, K: torch.Tensor, V: torch.Tensor, *, lens: Optional[torch.Tensor] = None,
+                         first_pos: Optional[torch.Tensor] = None, colsum: Optional[torch.Tensor] = None):
+        b, hq, hkv, d = self.shape
+        _need(K.dim() == 4, "K, V: [B, Hkv, n_rows, d]")
+        n, dev, i32 = K.shape[2], self.device, torch.int32
+        _call(dev, "d2o_paged_append", self.lib.d2o_paged_append, C.byref(self.cache), n,
+              _arg(K, "K", (b, hkv, n, d), self.dtype, dev), _arg(V, "V", (b, hkv, n, d), self.dtype, dev),
+              _arg(lens, "lens", (b,), i32, dev), _arg(first_pos, "first_pos", (b,), i32, dev),
+              _arg(colsum, "colsum", (b, hq, n), torch.float32, dev))
+
+    def d2o_paged_decode_step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, *,
+                              positions: Optional[torch.Tensor] = None, window: int = 0, n_sink: int = 0):
+        b, hq, hkv, d = self.shape
+        dev, dt = self.device, self.dtype
+        _call(dev, "d2o_paged_decode_step", self.lib.d2o_paged_decode_step, C.byref(self.cache), window, n_sink,
+              _arg(q, "q", (b, hq, d), dt, dev), _arg(k, "k", (b, hkv, d), dt, dev), _arg(v, "v", (b, hkv, d), dt, dev),
+              _arg(positions, "positions", (b,), torch.int32, dev), _arg(out, "out", (b, hq, d), dt, dev), *self._scratch)
+
+    def d2o_paged_evict(self, budgets: torch.Tensor, next_pos: torch.Tensor, *, n_sink: int = 0, window: int = 0):
+        b, _, hkv, _ = self.shape
+        _call(self.device, "d2o_paged_evict", self.lib.d2o_paged_evict, C.byref(self.cache),
+              _arg(budgets, "budgets", (b, hkv), torch.int32, self.device), _arg(next_pos, "next_pos", (b,), torch.int32, self.device),
+              n_sink, window, *self._scratch)
+
+    def check(self):
+        """Raises if a call on this cache has met a bad length or page number since the last check.  Synchronises."""
+        word, detail = self.status.tolist()
+        if word:
+            self.status.zero_()
+            _check(word, f"paged cache (detail {detail & 0xffffffff:#x})")

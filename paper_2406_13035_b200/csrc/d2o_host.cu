@@ -7,8 +7,10 @@
 
 #include <algorithm>
 
+#include "d2o_attention.cuh"
 #include "d2o_common.cuh"
 #include "d2o_decode.cuh"
+#include "d2o_paged.cuh"
 
 using namespace d2o;
 
@@ -578,6 +580,112 @@ extern "C" d2o_status d2o_full_decode_step(int32_t dtype, int32_t d_head, int32_
                                      (cudaStream_t)stream, &why);
   if (why != D2O_OK) return why;
   if (e != cudaSuccess) return cuda_fail(e, "launch_full_decode");
+  return D2O_OK;
+}
+
+// ------------------------------------------------------------------------------------ prompt attention, cache in pages
+extern "C" d2o_status d2o_prompt_attention(int32_t dtype, int32_t d_head, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
+                                           int32_t prompt_len, int32_t window, int32_t n_sink, const void* Q, const void* K,
+                                           const void* V, const int32_t* lens, void* out, float* lse, uint32_t* status,
+                                           void* stream) {
+  if (dtype != D2O_F32 && dtype != D2O_F16 && dtype != D2O_BF16) return D2O_ERR_UNSUPPORTED;
+  if (d_head != 64 && d_head != 128) return D2O_ERR_UNSUPPORTED;
+  if (batch < 1 || n_q_heads < 1 || n_kv_heads < 1 || prompt_len < 1 || window < 0 || n_sink < 0) return D2O_ERR_INVALID_ARG;
+  if (n_q_heads % n_kv_heads != 0) return D2O_ERR_INVALID_ARG;
+  if ((double)batch * n_q_heads * prompt_len >= 2147483648.0 || prompt_len > (1 << 20)) return D2O_ERR_UNSUPPORTED;
+  if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(out)) return D2O_ERR_INVALID_ARG;
+  if (((uintptr_t)lens & 3) || ((uintptr_t)lse & 3) || ((uintptr_t)status & 3)) return D2O_ERR_INVALID_ARG;
+  PromptAttentionArgs a;
+  a.Q = Q; a.K = K; a.V = V; a.lens = lens; a.out = out; a.lse = lse; a.status = status;
+  a.B = batch; a.Hq = n_q_heads; a.Hkv = n_kv_heads; a.P = prompt_len;
+  a.window = window > 0 ? std::min(window, prompt_len) : prompt_len;
+  a.n_sink = std::min(n_sink, prompt_len);
+  CUDA_TRY(launch_prompt_attention(dtype, d_head, a, (cudaStream_t)stream));
+  return D2O_OK;
+}
+
+// Sizes only; `view`: the pointers too.
+static d2o_status validate_paged(const d2o_paged_cache* c, PagedView* view) {
+  if (!c) return D2O_ERR_INVALID_ARG;
+  if (c->dtype != D2O_F32 && c->dtype != D2O_F16 && c->dtype != D2O_BF16) return D2O_ERR_UNSUPPORTED;
+  if (c->d_head != 64 && c->d_head != 128) return D2O_ERR_UNSUPPORTED;
+  if (c->batch < 1 || c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_pages < 1 || c->max_pages < 1) return D2O_ERR_INVALID_ARG;
+  if (c->n_q_heads % c->n_kv_heads != 0) return D2O_ERR_INVALID_ARG;
+  const int g = c->n_q_heads / c->n_kv_heads;
+  if (g != 1 && g != 2 && g != 4 && g != 8) return D2O_ERR_UNSUPPORTED;
+  if (c->page_size < kPagedTile || c->page_size > 1024 || (c->page_size & (c->page_size - 1))) return D2O_ERR_UNSUPPORTED;
+  if ((double)c->n_pages * c->n_kv_heads * c->page_size >= 2147483648.0) return D2O_ERR_UNSUPPORTED;
+  if ((double)c->batch * c->n_kv_heads > 65535.0 || (double)c->max_pages * c->page_size >= 1073741824.0) return D2O_ERR_UNSUPPORTED;
+  if ((c->pos == nullptr) != (c->score == nullptr)) return D2O_ERR_INVALID_ARG;
+  if (!view) return D2O_OK;
+  if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || !c->page_table || !c->len) return D2O_ERR_INVALID_ARG;
+  if (((uintptr_t)c->pos | (uintptr_t)c->score | (uintptr_t)c->page_table | (uintptr_t)c->len | (uintptr_t)c->status) & 3)
+    return D2O_ERR_INVALID_ARG;
+  view->k = c->k_pages; view->v = c->v_pages; view->pos = c->pos; view->score = c->score;
+  view->table = c->page_table; view->len = c->len; view->status = c->status;
+  view->B = c->batch; view->Hq = c->n_q_heads; view->Hkv = c->n_kv_heads;
+  view->n_pages = c->n_pages; view->max_pages = c->max_pages;
+  view->page_shift = 0;
+  while ((1 << view->page_shift) < c->page_size) ++view->page_shift;
+  return D2O_OK;
+}
+
+static size_t paged_scratch_bytes(const d2o_paged_cache* c) {
+  return PagedScratch(c->batch * c->n_kv_heads, c->n_q_heads / c->n_kv_heads, c->d_head,
+                      (size_t)c->n_pages * c->n_kv_heads * c->page_size, c->score != nullptr).end;
+}
+
+extern "C" d2o_status d2o_paged_workspace_size(const d2o_paged_cache* cache, size_t* bytes) {
+  const d2o_status st = validate_paged(cache, nullptr);
+  if (st != D2O_OK) return st;
+  if (!bytes) return D2O_ERR_INVALID_ARG;
+  *bytes = paged_scratch_bytes(cache);
+  return D2O_OK;
+}
+
+static d2o_status validate_scratch(const d2o_paged_cache* c, const void* scratch, size_t bytes) {
+  if (!scratch) return D2O_ERR_INVALID_ARG;
+  return ((uintptr_t)scratch & 255) || bytes < paged_scratch_bytes(c) ? D2O_ERR_WORKSPACE : D2O_OK;
+}
+
+extern "C" d2o_status d2o_paged_append(const d2o_paged_cache* cache, int32_t n_rows, const void* K, const void* V,
+                                       const int32_t* lens, const int32_t* first_pos, const float* colsum, void* stream) {
+  PagedView p;
+  const d2o_status st = validate_paged(cache, &p);
+  if (st != D2O_OK) return st;
+  if (n_rows < 1 || !aligned16(K) || !aligned16(V)) return D2O_ERR_INVALID_ARG;
+  if ((first_pos || colsum) && !p.pos) return D2O_ERR_INVALID_ARG;
+  if (((uintptr_t)lens | (uintptr_t)first_pos | (uintptr_t)colsum) & 3) return D2O_ERR_INVALID_ARG;
+  CUDA_TRY(launch_paged_append(p, cache->dtype, cache->d_head, n_rows, K, V, lens, first_pos, colsum, (cudaStream_t)stream));
+  return D2O_OK;
+}
+
+extern "C" d2o_status d2o_paged_decode_step(const d2o_paged_cache* cache, int32_t window, int32_t n_sink, const void* q,
+                                            const void* k, const void* v, const int32_t* positions, void* out, void* scratch,
+                                            size_t scratch_bytes, void* stream) {
+  PagedView p;
+  d2o_status st = validate_paged(cache, &p);
+  if (st != D2O_OK) return st;
+  if (window < 0 || n_sink < 0 || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return D2O_ERR_INVALID_ARG;
+  if (((uintptr_t)positions & 3) || (positions && !p.pos)) return D2O_ERR_INVALID_ARG;
+  st = validate_scratch(cache, scratch, scratch_bytes);
+  if (st != D2O_OK) return st;
+  CUDA_TRY(launch_paged_decode(p, cache->dtype, cache->d_head, window, n_sink, q, k, v, positions, out, (char*)scratch,
+                               (cudaStream_t)stream));
+  return D2O_OK;
+}
+
+extern "C" d2o_status d2o_paged_evict(const d2o_paged_cache* cache, const int32_t* budgets, const int32_t* next_pos,
+                                      int32_t n_sink, int32_t window, void* scratch, size_t scratch_bytes, void* stream) {
+  PagedView p;
+  d2o_status st = validate_paged(cache, &p);
+  if (st != D2O_OK) return st;
+  if (!budgets || !next_pos || (((uintptr_t)budgets | (uintptr_t)next_pos) & 3) || n_sink < 0 || window < 0 || !p.pos)
+    return D2O_ERR_INVALID_ARG;
+  st = validate_scratch(cache, scratch, scratch_bytes);
+  if (st != D2O_OK) return st;
+  CUDA_TRY(launch_paged_evict(p, cache->dtype, cache->d_head, budgets, next_pos, n_sink, window, (char*)scratch,
+                              (cudaStream_t)stream));
   return D2O_OK;
 }
 

@@ -1,0 +1,325 @@
+// A key-value cache in pages: filling it, and evicting from it by accumulated attention weight (Eq. 6-8).
+//
+//   append_kernel   rows of a prompt or a turn -> pages, with positions and scores
+//   evict_kernel    which rows stay (radix select over the cluster of a slice), and the moves that close the gaps
+#include <cooperative_groups.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "d2o_common.cuh"
+#include "d2o_paged.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace d2o {
+
+// ------------------------------------------------------------------------------------ append
+constexpr int kAppendThreads = 256;
+constexpr int kAppendRows = 64;              // rows per CTA
+
+struct AppendArgs {
+  PagedView p;
+  const char *K, *V;                         // [B, Hkv, n_rows, row bytes]
+  const int32_t *lens, *first_pos;
+  const float* colsum;                       // [B, Hq, n_rows]
+  int n_rows;
+};
+
+// A copy: bound by HBM, each byte read and written once.  A group of lanes takes one row's 16-byte pieces of K and V, four rows
+// in flight.
+template <int ROWB>
+__global__ void __launch_bounds__(kAppendThreads)
+append_kernel(AppendArgs a) {
+  start_dependents();
+  wait_for_prior_grid();
+  constexpr int LPR = ROWB / 16, GRPS = kAppendThreads / LPR, U = kAppendRows / GRPS < 4 ? kAppendRows / GRPS : 4;
+  const PagedView& p = a.p;
+  const int sl = blockIdx.y, b = sl / p.Hkv, h = sl % p.Hkv;
+  const int held = p.len[sl];
+  if (held < 0) return;
+  const int n = a.lens ? min(a.lens[b], a.n_rows) : a.n_rows;
+  const int i0 = blockIdx.x * kAppendRows, grp = threadIdx.x / LPR, lig = threadIdx.x % LPR;
+  const long long reach = p.reach();
+  auto place = [&](int i) {                                  // pool row of row i; -1: none
+    const long long r = (long long)held + i;
+    if (r >= reach) { p.report(kPagedShortTable); return -1; }
+    const int row0 = p.page_row0(b, h, (int)r);
+    if (row0 < 0) { p.report(kPagedBadPage); return -1; }
+    return row0 + p.in_page((int)r);
+  };
+  const size_t src = ((size_t)sl * a.n_rows + i0) * ROWB + lig * 16;
+#pragma unroll
+  for (int base = 0; base < kAppendRows; base += U * GRPS) {
+    uint4 kv[U], vv[U];
+    int to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = base + u * GRPS + grp;
+      to[u] = -1;
+      if (i0 + i < n) {
+        kv[u] = ld_stream_v4(a.K + src + (size_t)i * ROWB);
+        vv[u] = ld_stream_v4(a.V + src + (size_t)i * ROWB);
+        to[u] = place(i0 + i);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (to[u] >= 0) {
+        *reinterpret_cast<uint4*>((char*)p.k + (size_t)to[u] * ROWB + lig * 16) = kv[u];
+        *reinterpret_cast<uint4*>((char*)p.v + (size_t)to[u] * ROWB + lig * 16) = vv[u];
+      }
+  }
+  const int i = i0 + threadIdx.x;
+  if (p.pos && threadIdx.x < kAppendRows && i < n) {
+    const int to = place(i);
+    if (to >= 0) {
+      p.pos[to] = (a.first_pos ? a.first_pos[b] : 0) + i;
+      float s = 0.f;
+      if (a.colsum) {
+        const int G = p.Hq / p.Hkv;
+        const float* c = a.colsum + ((size_t)b * p.Hq + (size_t)h * G) * a.n_rows + i;
+        s = c[0];
+        for (int g = 1; g < G; ++g) s += c[(size_t)g * a.n_rows];
+      }
+      p.score[to] = s;
+    }
+  }
+}
+
+cudaError_t launch_paged_append(const PagedView& p, int dtype, int D, int n_rows, const void* K, const void* V, const int32_t* lens,
+                                const int32_t* first_pos, const float* colsum, cudaStream_t st) {
+  AppendArgs a = {p, (const char*)K, (const char*)V, lens, first_pos, colsum, n_rows};
+  const int rowb = D * (dtype == D2O_F32 ? 4 : 2);
+  // x: chunks of rows (up to 2^31), y: slices, at most 65535 of them per launch (checked by the caller)
+  const dim3 grid((unsigned)((n_rows + kAppendRows - 1) / kAppendRows), (unsigned)(p.B * p.Hkv));
+  return rowb == 128 ? launch_behind(append_kernel<128>, grid, kAppendThreads, 0, st, a)
+       : rowb == 256 ? launch_behind(append_kernel<256>, grid, kAppendThreads, 0, st, a)
+                     : launch_behind(append_kernel<512>, grid, kAppendThreads, 0, st, a);
+}
+
+// ------------------------------------------------------------------------------------ evict
+constexpr int kEvictThreads = 512;
+constexpr int kEvictItems = 4;               // consecutive rows per thread in the ordered pass
+constexpr int kEvictKeys = 12288;            // rows of a CTA whose keys stay in shared memory
+constexpr int kEvictMaxCluster = 8;
+
+struct EvictArgs {
+  PagedView p;
+  const int32_t *budgets, *next_pos;         // [B, Hkv], [B]
+  int2* moves;                               // per row of the pools: (from, to) of the move with that number, as pool rows
+  int n_sink, window;
+};
+
+// A row's rank among the rows of its slice is decided by a key, then by the position (earlier is higher).  Keys: protected rows
+// above all, then NaN, then the scores in their order.
+__device__ __forceinline__ uint32_t evict_key(float score, int pos, int n_sink, long long first_recent) {
+  if (pos < n_sink || pos >= first_recent) return 0xffffffffu;
+  if (score != score) return 0xfffffffeu;
+  return float_ord(score + 0.f);                             // -0 + 0 = +0
+}
+
+struct EvictExchange {                       // read by the other CTAs of the cluster
+  int hist[2][256];
+  int holes, movers, bad;
+};
+
+// One cluster per slice, its rows divided evenly over the CTAs.  (1) Keys.  (2) Radix select, 8 bits per round, of the lowest
+// key that stays: each CTA counts its rows, all add up the counts of all.  Where rows of that key stay only in part, rounds
+// over the positions of those follow (few slices have such ties, and then in a round or two a handful of rows).  (3) The rows below
+// the budget that go and the rows behind it that stay, each numbered in ascending order, form the moves; as many of one as of
+// the other, and sources and targets do not overlap, so that all moves run at once.  (4) The moves, divided over the
+// cluster.  What costs are the dependent steps: three or four cluster barriers for the select, two for the numbering.
+template <int ROWB>
+__global__ void __launch_bounds__(kEvictThreads)
+evict_kernel(EvictArgs a) {
+  start_dependents();
+  wait_for_prior_grid();
+  constexpr int LPR = ROWB / 16, GRPS = kEvictThreads / LPR;
+  extern __shared__ __align__(16) uint32_t s_keys[];
+  __shared__ EvictExchange x;
+  __shared__ int s_warp[32], s_total, s_bin, s_need, s_count;
+  cg::cluster_group cluster = cg::this_cluster();
+  const PagedView& p = a.p;
+  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int sl = blockIdx.x / C, b = sl / p.Hkv, h = sl % p.Hkv;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int n = p.len[sl], budget = a.budgets[sl];
+  // the same for all CTAs of the cluster
+  if (n < 0) return;
+  if (n > p.reach()) { if (tid == 0) p.report(kPagedShortTable); return; }
+  if (budget < 0) { if (tid == 0) p.report(kPagedBadBudget); return; }
+  if (n <= budget || budget == 0) return;
+  const long long first_recent = (long long)a.next_pos[b] - a.window;
+  const int chunk = (n + C - 1) / C, r0 = min(n, rank * chunk), m = min(n, r0 + chunk) - r0;      // this CTA's rows r0 .. r0 + m
+  if (tid < 256) { x.hist[0][tid] = 0; x.hist[1][tid] = 0; }
+  if (tid == 0) { x.holes = x.movers = x.bad = 0; }
+  __syncthreads();
+  auto pool_row = [&](int r) { const int row0 = p.page_row0(b, h, r); return row0 < 0 ? -1 : row0 + p.in_page(r); };
+  auto load_key = [&](int r) {
+    const int at = pool_row(r);
+    if (at < 0) { x.bad = 1; return 0u; }
+    return evict_key(p.score[at], p.pos[at], a.n_sink, first_recent);
+  };
+  auto key = [&](int i) { return i < kEvictKeys ? s_keys[i] : load_key(r0 + i); };
+  for (int i = tid; i < m; i += kEvictThreads) {
+    const uint32_t k = load_key(r0 + i);
+    if (i < kEvictKeys) s_keys[i] = k;
+  }
+  __syncthreads();
+  // ---- the lowest (key, position) that stays, from the top eight bits down
+  uint32_t kth = 0, inv_pos = 0;                             // rows above (kth, inv_pos), or equal, stay
+  int need = budget;
+  bool by_pos = false;
+  int round = 0;
+  auto select = [&](auto&& value, bool& exact) {             // 32 bits; value(i, v): is row i still in question, and its bits
+    uint32_t prefix = 0, mask = 0;
+    exact = false;
+    for (int shift = 24; shift >= 0; shift -= 8, ++round) {
+      int* hist = x.hist[round & 1];
+      for (int i = tid; i < m; i += kEvictThreads) {
+        uint32_t v;
+        if (value(i, v) && (v & mask) == prefix) atomicAdd(&hist[(v >> shift) & 255], 1);
+      }
+      cluster.sync();
+      int c = 0;
+      if (tid < 256)
+        for (int r = 0; r < C; ++r) c += cluster.map_shared_rank(&x, r)->hist[round & 1][255 - tid];       // highest bin first
+      // inclusive prefix over the 256 bins: eight warps
+      int inc = c;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += t; }
+      if (lane == 31 && warp < 8) s_warp[warp] = inc;
+      x.hist[(round + 1) & 1][tid & 255] = 0;                // read by all before the barrier above
+      __syncthreads();
+      if (tid < 256) {
+        for (int w = 0; w < warp; ++w) inc += s_warp[w];
+        if (inc >= need && inc - c < need) { s_bin = 255 - tid; s_need = need - (inc - c); s_count = c; }
+      }
+      __syncthreads();
+      prefix |= (uint32_t)s_bin << shift; mask |= 255u << shift;
+      need = s_need;
+      if (need == s_count) { exact = true; ++round; break; }     // all rows of this bin stay: the lower bits do not matter
+    }
+    return prefix;
+  };
+  bool exact;
+  kth = select([&](int i, uint32_t& v) { v = key(i); return true; }, exact);
+  bool bad = false;
+  for (int r = 0; r < C; ++r) bad |= cluster.map_shared_rank(&x, r)->bad != 0;
+  if (bad) {                                                 // the same for all
+    if (tid == 0 && rank == 0) p.report(kPagedBadPage);
+    cluster.sync();                                          // our exchange area may still be read
+    return;
+  }
+  if (!exact) {
+    by_pos = true;
+    inv_pos = select([&](int i, uint32_t& v) {
+      if (key(i) != kth) return false;
+      v = ~(uint32_t)p.pos[pool_row(r0 + i)];
+      return true;
+    }, exact);
+  }
+  auto stays = [&](int i) {
+    const uint32_t k = key(i);
+    if (!by_pos || k != kth) return k >= kth;
+    return ~(uint32_t)p.pos[pool_row(r0 + i)] >= inv_pos;
+  };
+  // ---- number the rows below the budget that go (holes) and those behind it that stay (movers)
+  auto numbered = [&](auto&& hole, auto&& mover) {
+    int holes = 0, movers = 0;
+    for (int base = 0; base < m; base += kEvictItems * kEvictThreads) {
+      int is_hole = 0, is_mover = 0;
+#pragma unroll
+      for (int e = 0; e < kEvictItems; ++e) {
+        const int i = base + tid * kEvictItems + e;
+        if (i >= m) break;
+        const bool s = stays(i);
+        if (r0 + i < budget) { if (!s) is_hole |= 1 << e; }
+        else if (s) is_mover |= 1 << e;
+      }
+      // exclusive prefix over the block of both counts at once (each at most 2048)
+      const int mine = __popc(is_hole) | (__popc(is_mover) << 16);
+      int inc = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += t; }
+      __syncthreads();
+      if (lane == 31) s_warp[warp] = inc;
+      __syncthreads();
+      if (warp == 0) {
+        const int w = lane < kEvictThreads / 32 ? s_warp[lane] : 0;
+        int winc = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, winc, o); if (lane >= o) winc += t; }
+        s_warp[lane] = winc - w;
+        if (lane == 31) s_total = winc;
+      }
+      __syncthreads();
+      const int before = inc - mine + s_warp[warp];
+      int nh = holes + (before & 0xffff), nm = movers + (before >> 16);
+#pragma unroll
+      for (int e = 0; e < kEvictItems; ++e) {
+        const int r = r0 + base + tid * kEvictItems + e;
+        if (is_hole >> e & 1) hole(nh++, r);
+        if (is_mover >> e & 1) mover(nm++, r);
+      }
+      holes += s_total & 0xffff; movers += s_total >> 16;
+    }
+    if (tid == 0) { x.holes = holes; x.movers = movers; }
+  };
+  numbered([](int, int) {}, [](int, int) {});
+  cluster.sync();
+  int h0 = 0, m0 = 0, nh = 0, nm = 0;
+  for (int r = 0; r < C; ++r) {
+    const EvictExchange* y = cluster.map_shared_rank(&x, r);
+    if (r < rank) { h0 += y->holes; m0 += y->movers; }
+    nh += y->holes; nm += y->movers;
+  }
+  cluster.sync();                                            // before the counts are written again
+  const int moves = min(nh, nm);                             // equal, unless positions stand twice
+  numbered([&](int k, int r) { if (h0 + k < moves) a.moves[pool_row(h0 + k)].y = pool_row(r); },
+           [&](int k, int r) { if (m0 + k < moves) a.moves[pool_row(m0 + k)].x = pool_row(r); });
+  cluster.sync();
+  // ---- the moves
+  const int grp = tid / LPR, lig = tid % LPR;
+  for (int k = rank * GRPS + grp; k < moves; k += C * GRPS) {
+    const int2 mv = a.moves[pool_row(k)];
+    const size_t from = (size_t)mv.x * ROWB + lig * 16, to = (size_t)mv.y * ROWB + lig * 16;
+    const uint4 kv = ld_stream_v4((const char*)p.k + from), vv = ld_stream_v4((const char*)p.v + from);
+    *reinterpret_cast<uint4*>((char*)p.k + to) = kv;
+    *reinterpret_cast<uint4*>((char*)p.v + to) = vv;
+    if (lig == 0) { p.pos[mv.y] = p.pos[mv.x]; p.score[mv.y] = p.score[mv.x]; }
+  }
+}
+
+template <int ROWB>
+static cudaError_t launch_evict(const EvictArgs& a, int n_slices, int C, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(evict_kernel<ROWB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictKeys * 4);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(n_slices * C)); cfg.blockDim = dim3(kEvictThreads); cfg.dynamicSmemBytes = kEvictKeys * 4; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, evict_kernel<ROWB>, a);
+}
+
+cudaError_t launch_paged_evict(const PagedView& p, int dtype, int D, const int32_t* budgets, const int32_t* next_pos, int n_sink,
+                               int window, char* scratch, cudaStream_t st) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return cudaGetLastError();
+  const int n_slices = p.B * p.Hkv;
+  const PagedScratch s(n_slices, p.Hq / p.Hkv, D, (size_t)p.n_pages * p.Hkv << p.page_shift, true);
+  const EvictArgs a = {p, budgets, next_pos, reinterpret_cast<int2*>(scratch + s.rows), n_sink, window};
+  int C = 1;                                                 // one wave of clusters
+  while (2 * C <= kEvictMaxCluster && (long)n_slices * 2 * C <= 2l * sms) C *= 2;
+  const int rowb = D * (dtype == D2O_F32 ? 4 : 2);
+  return rowb == 128 ? launch_evict<128>(a, n_slices, C, st) : rowb == 256 ? launch_evict<256>(a, n_slices, C, st)
+                                                                           : launch_evict<512>(a, n_slices, C, st);
+}
+
+}  // namespace d2o

@@ -1,0 +1,487 @@
+"""A cache in pages (d2o_paged_append, d2o_paged_decode_step, d2o_paged_evict) against plain statements of the formulas in
+float64 on the host, and the three in a row as a serving program uses them.
+
+Every test compares whole pools: what a call does not own must keep its bits, and all of it holds NaN at first, so that a row
+read where nothing was put shows.  Rows and positions are compared exactly.
+
+Tolerance of the attention.  A logit errs by a few 2^-24 of the magnitudes that it sums: delta = 16 * 2^-24 * max_j sum_e |q_e
+k_je| / sqrt(d).  A weight is off by a factor of at most 1 + 2 delta (itself, the sum), and by 2^-20 from exp2, the joins and, for
+16-bit caches, the two 16-bit terms in which it enters the products (bf16: 2^-16 more).  An output is the rounding of something
+within e = (2 delta + 2^-20 + 2^-16) * sum_j p_j |v_j| of the reference (fp32 and fp16: without 2^-16); a score is off by 2 delta +
+2^-20 of the added weight, and by the rounding of the sum."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_13035_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+NAN = float("nan")
+
+
+def bits(t):
+    return t.detach().cpu().contiguous().view({4: torch.int32, 2: torch.int16}[t.element_size()]).numpy()
+
+
+class Paged:
+    """A cache, its pools full of NaN, with `spare` pages that no table names; a host copy of what should be in it."""
+
+    def __init__(self, seed, b, hq, hkv, d, dtype, page, max_pages, lens, scored=True, spare=2):
+        self.g = torch.Generator().manual_seed(seed)
+        self.b, self.hq, self.hkv, self.d, self.page, self.dt, self.dtype = b, hq, hkv, d, page, DT[dtype], dtype
+        n_pages = b * max_pages + spare
+        self.table = torch.randperm(n_pages, generator=self.g)[: b * max_pages].view(b, max_pages).to(torch.int32)
+        self.len = torch.as_tensor(lens, dtype=torch.int32)
+        if self.len.dim() == 1:
+            self.len = self.len[:, None].expand(b, hkv).contiguous()
+        shape = (n_pages, hkv, page)
+        self.k, self.v = torch.full((*shape, d), NAN, dtype=self.dt), torch.full((*shape, d), NAN, dtype=self.dt)
+        self.pos = torch.full(shape, -7, dtype=torch.int32) if scored else None
+        self.score = torch.full(shape, NAN) if scored else None
+        reach = max_pages * page
+        for i in range(b):
+            for h in range(hkv):
+                for r in range(min(int(self.len[i, h]), reach)):
+                    pg, at = self.at(i, r)
+                    self.k[pg, h, at] = torch.randn(d, generator=self.g).to(self.dt)
+                    self.v[pg, h, at] = torch.randn(d, generator=self.g).to(self.dt)
+                    if scored:
+                        self.pos[pg, h, at], self.score[pg, h, at] = r, float(torch.rand(1, generator=self.g))
+        self.upload()
+
+    def upload(self):
+        dev = lambda t: None if t is None else t.cuda()
+        self.dk, self.dv, self.dpos, self.dscore, self.dtable, self.dlen = map(dev, (self.k, self.v, self.pos, self.score, self.table, self.len))
+        self.cache = B.D2OPagedCache(self.dk, self.dv, self.dtable, self.dlen, n_q_heads=self.hq, pos=self.dpos, score=self.dscore)
+
+    def at(self, i, r):
+        return int(self.table[i, r // self.page]), r % self.page
+
+    def randn(self, *s):
+        return torch.randn(*s, generator=self.g).to(self.dt)
+
+    def rows(self, pool, i, h, rs):
+        return torch.stack([pool[self.at(i, r)[0], h, self.at(i, r)[1]] for r in rs]) if len(rs) else pool.new_zeros(0, *pool.shape[3:])
+
+    def same(self, scores=True):
+        """The device's pools are the host's, bit for bit."""
+        for name, host, dev in (("k", self.k, self.dk), ("v", self.v, self.dv), ("pos", self.pos, self.dpos), ("score", self.score, self.dscore)):
+            if host is not None and (scores or name != "score"):
+                assert np.array_equal(bits(host), bits(dev)), name
+        assert torch.equal(self.len, self.dlen.cpu()) and torch.equal(self.table, self.dtable.cpu())
+
+    # ---- the plain statements
+    def append(self, K, V, lens=None, first=None, colsum=None):
+        n = K.shape[2]
+        for i in range(self.b):
+            for h in range(self.hkv):
+                for j in range(min(n, n if lens is None else int(lens[i])) if self.len[i, h] >= 0 else 0):
+                    pg, at = self.at(i, int(self.len[i, h]) + j)
+                    self.k[pg, h, at], self.v[pg, h, at] = K[i, h, j], V[i, h, j]
+                    if self.pos is not None:
+                        self.pos[pg, h, at] = (0 if first is None else int(first[i])) + j
+                        s = torch.zeros(())
+                        if colsum is not None:
+                            G = self.hq // self.hkv
+                            s = colsum[i, h * G, j]
+                            for g in range(1, G):
+                                s = s + colsum[i, h * G + g, j]
+                        self.score[pg, h, at] = s
+
+    def step(self, q, k, v, out, positions, window, n_sink):
+        """Checks `out` and the device's scores, and takes the scores over (they are sums of rounded terms)."""
+        G = self.hq // self.hkv
+        got_scores = None if self.score is None else self.dscore.cpu()
+        for i in range(self.b):
+            for h in range(self.hkv):
+                t = int(self.len[i, h])
+                if t < 0:
+                    assert bool((out[i, h * G:(h + 1) * G] == 3).all())
+                    continue
+                pg, at = self.at(i, t)
+                self.k[pg, h, at], self.v[pg, h, at] = k[i, h], v[i, h]
+                rs = [r for r in range(t + 1) if window == 0 or r > t - window or r < n_sink]
+                K, V = self.rows(self.k, i, h, rs).double(), self.rows(self.v, i, h, rs).double()
+                Q = q[i, h * G:(h + 1) * G].double()
+                p = torch.softmax(Q @ K.T / math.sqrt(self.d), -1)
+                delta = 16 * 2.0 ** -24 * float((Q.abs() @ K.abs().T).max()) / math.sqrt(self.d)
+                w = 2 * delta + 2.0 ** -20
+                ref, e = p @ V, (w + (2.0 ** -16 if self.dtype == "bf16" else 0)) * (p @ V.abs())
+                o = out[i, h * G:(h + 1) * G].cpu().double()
+                ok = ((ref - e).to(self.dt).double() <= o) & (o <= (ref + e).to(self.dt).double())
+                assert bool(ok.all()), (i, h, float(((o - ref).abs() / e).max()))
+                if self.score is not None:
+                    self.pos[pg, h, at] = t if positions is None else int(positions[i])
+                    add = p.sum(0)
+                    for r, x in zip(rs, add.tolist()):
+                        pr, ar = self.at(i, r)
+                        was = 0.0 if r == t else float(self.score[pr, h, ar])
+                        now = float(got_scores[pr, h, ar])
+                        assert abs(now - (was + x)) <= w * x + 2.0 ** -24 * abs(was + x), (i, h, r)
+                        self.score[pr, h, ar] = now
+
+    def evict(self, budgets, next_pos, n_sink, window):
+        for i in range(self.b):
+            for h in range(self.hkv):
+                n, s = int(self.len[i, h]), int(budgets[i, h])
+                if n < 0 or n <= s or s < 0:
+                    continue
+                pos = self.rows(self.pos, i, h, range(n)).tolist()
+                score = self.rows(self.score, i, h, range(n)).tolist()
+
+                def rank(r):
+                    protected = pos[r] < n_sink or pos[r] >= int(next_pos[i]) - window
+                    nan = score[r] != score[r]
+                    return (not protected, protected is False and not nan, 0 if protected or nan else -score[r], pos[r])
+                kept = sorted(sorted(range(n), key=rank)[:s])
+                holes = [r for r in range(s) if r not in set(kept)]
+                movers = [r for r in kept if r >= s]
+                assert len(holes) == len(movers)
+                for to, frm in zip(holes, movers):
+                    (tp, ta), (fp, fa) = self.at(i, to), self.at(i, frm)
+                    for pool in (self.k, self.v, self.pos, self.score):
+                        pool[tp, h, ta] = pool[fp, h, fa]
+
+
+# ---------------------------------------------------------------------------------------------- append
+@pytest.mark.parametrize("b,hq,hkv,d,dtype,page,n,lens,held,scored", [
+    (1, 1, 1, 64, "f32", 16, 1, None, [0], True), (2, 4, 2, 128, "bf16", 16, 5, [5, 0], [15, 16], True),
+    (3, 8, 2, 128, "f16", 32, 70, [70, 33, 1], [0, 31, 7], True), (2, 2, 2, 64, "bf16", 64, 130, None, [63, -1], False),
+    (2, 16, 2, 128, "f32", 16, 65, [200, 64], [1, 2], True), (1, 3, 3, 64, "f16", 1024, 64, [-3], [5], False)])
+def test_append(cuda_device, b, hq, hkv, d, dtype, page, n, lens, held, scored):
+    c = Paged(n, b, hq, hkv, d, dtype, page, (n + max(held) + page - 1) // page + 1, held, scored)
+    K, V = c.randn(b, hkv, n, d), c.randn(b, hkv, n, d)
+    first = torch.arange(b, dtype=torch.int32) * 1000 + 5 if scored else None
+    colsum = torch.rand(b, hq, n, generator=c.g) if scored else None
+    up = lambda t: None if t is None else t.cuda()
+    li = None if lens is None else torch.tensor(lens, dtype=torch.int32)
+    c.cache.d2o_paged_append(K.cuda(), V.cuda(), lens=up(li), first_pos=up(first), colsum=up(colsum))
+    c.append(K, V, li, first, colsum)
+    c.same()
+    if scored:                                                                 # defaults: positions from 0, scores 0
+        c.cache.d2o_paged_append(K.cuda(), V.cuda(), lens=up(li))
+        c.append(K, V, li)
+        c.same()
+    c.cache.check()
+
+
+# ---------------------------------------------------------------------------------------------- decode
+STEPS = [  # batch, q heads, kv heads, d, page, rows held, window, sinks, scores
+    (1, 1, 1, 64, 16, [0], 0, 0, True), (1, 2, 1, 128, 16, [1], 0, 0, True), (2, 4, 1, 128, 16, [15, 16], 0, 0, True),
+    (3, 8, 1, 64, 32, [17, 31, 47], 0, 0, True), (2, 8, 2, 128, 64, [300, 3], 0, 0, True), (1, 4, 4, 64, 1024, [700], 0, 0, False),
+    (4, 4, 2, 128, 16, [100, -1, 0, 255], 0, 0, True), (2, 2, 2, 128, 16, [200, 90], 1, 0, True), (2, 2, 1, 64, 16, [200, 90], 33, 0, True),
+    (3, 4, 2, 128, 32, [500, 40, 64], 64, 4, True), (2, 8, 1, 128, 16, [600, 100], 100, 17, True), (1, 4, 1, 64, 128, [900], 500, 300, True),
+    (1, 4, 1, 128, 16, [64], 1000, 4, False), (1, 16, 2, 128, 64, [1700], 0, 0, True), (40, 4, 4, 64, 16, list(range(0, 120, 3)), 0, 0, True),
+    (300, 2, 1, 64, 16, [7] * 299 + [333], 0, 0, False)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("b,hq,hkv,d,page,held,window,sinks,scored", STEPS)
+def test_decode_step(cuda_device, b, hq, hkv, d, page, held, window, sinks, scored, dtype):
+    """Two steps in a row, the lengths advanced in between as the caller does."""
+    c = Paged(sum(held) + window, b, hq, hkv, d, dtype, page, (max(held) + 2 + page - 1) // page, held, scored)
+    for step in range(2):
+        q, k, v = c.randn(b, hq, d), c.randn(b, hkv, d), c.randn(b, hkv, d)
+        positions = torch.arange(b, dtype=torch.int32) + 9000 if scored and step else None
+        out = torch.full((b, hq, d), 3.0, dtype=c.dt, device="cuda")
+        c.cache.d2o_paged_decode_step(q.cuda(), k.cuda(), v.cuda(), out, positions=None if positions is None else positions.cuda(),
+                                      window=window, n_sink=sinks)
+        c.step(q, k, v, out, positions, window, sinks)
+        c.same()
+        c.cache.check()
+        c.len += (c.len >= 0).to(torch.int32)
+        c.dlen.copy_(c.len)
+
+
+def test_decode_heads_of_different_lengths(cuda_device):
+    c = Paged(1, 2, 4, 2, 128, "bf16", 16, 8, [[5, 90], [33, -1]])
+    q, k, v = c.randn(2, 4, 128), c.randn(2, 2, 128), c.randn(2, 2, 128)
+    out = torch.full((2, 4, 128), 3.0, dtype=c.dt, device="cuda")
+    c.cache.d2o_paged_decode_step(q.cuda(), k.cuda(), v.cuda(), out)
+    c.step(q, k, v, out, None, 0, 0)
+    c.same()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_decode_shared_prefix(cuda_device, dtype):
+    """Two sequences with the same first pages, without scores."""
+    c = Paged(2, 2, 4, 2, 64, dtype, 16, 6, [70, 83], scored=False)
+    for r in range(48):
+        for h in range(2):
+            for pool in (c.k, c.v):
+                pool[c.at(1, r)[0], h, c.at(1, r)[1]] = NAN
+    c.table[1, :3] = c.table[0, :3]
+    c.upload()
+    q, k, v = c.randn(2, 4, 64), c.randn(2, 2, 64), c.randn(2, 2, 64)
+    out = torch.full((2, 4, 64), 3.0, dtype=c.dt, device="cuda")
+    c.cache.d2o_paged_decode_step(q.cuda(), k.cuda(), v.cuda(), out)
+    c.step(q, k, v, out, None, 0, 0)
+    c.same()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_decode_long(cuda_device, dtype):
+    """40000 rows over every SM, made and checked on the GPU: logits of variance 1, so that every row counts."""
+    n, page, d, hkv, G = 40000, 64, 128, 2, 4
+    g = torch.Generator(device="cuda").manual_seed(1)
+    per = (n + page) // page
+    table = torch.randperm(per + 1, generator=g, device="cuda")[:per].to(torch.int32)[None].contiguous()
+    kp, vp = (torch.randn(per + 1, hkv, page, d, generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    pos, score = torch.zeros(per + 1, hkv, page, dtype=torch.int32, device="cuda"), torch.zeros(per + 1, hkv, page, device="cuda")
+    length = torch.full((1, hkv), n, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(1, h, d, generator=g, device="cuda").to(DT[dtype]) for h in (hkv * G, hkv, hkv))
+    out = torch.empty_like(q)
+    c = B.D2OPagedCache(kp, vp, table, length, n_q_heads=hkv * G, pos=pos, score=score)
+    c.d2o_paged_decode_step(q, k, v, out)
+    again = torch.empty_like(q)
+    first = score.clone()
+    c.d2o_paged_decode_step(q, k, v, again)
+    assert torch.equal(out, again)
+    for h in range(hkv):
+        rows = lambda pool: pool[table[0].long()].transpose(0, 1).flatten(1, 2)[h, :n + 1].double()
+        K, V, Q = rows(kp), rows(vp), q[0, h * G:(h + 1) * G].double()
+        assert torch.equal(K[n], k[0, h].double()) and torch.equal(V[n], v[0, h].double())
+        p = torch.softmax(Q @ K.T / math.sqrt(d), -1)
+        w = 32 * 2.0 ** -24 * float((Q.abs() @ K.abs().T).max()) / math.sqrt(d) + 2.0 ** -20
+        e = (w + (2.0 ** -16 if dtype == "bf16" else 0)) * (p @ V.abs())
+        ref, o = p @ V, out[0, h * G:(h + 1) * G].double()
+        assert bool((((ref - e).to(DT[dtype]).double() <= o) & (o <= (ref + e).to(DT[dtype]).double())).all())
+        s = first[table[0].long()].transpose(0, 1).flatten(1, 2)[h, :n + 1].double()
+        assert bool(((s - p.sum(0)).abs() <= (w + 2.0 ** -24) * p.sum(0)).all())
+    c.check()
+
+
+def test_decode_offsets_past_32_bits(cuda_device):
+    """A pool of more than 2^31 elements, and rows of it behind that border."""
+    page, d, hkv, dt = 1024, 128, 8, torch.bfloat16
+    n_pages = (1 << 31) // (page * d * hkv) + 8
+    kp = torch.zeros(n_pages, hkv, page, d, dtype=dt, device="cuda")
+    vp = torch.zeros_like(kp)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 3]], dtype=torch.int32, device="cuda")
+    for p in table[0].tolist():
+        kp[p], vp[p] = (torch.randn(hkv, page, d, generator=g, device="cuda").to(dt) for _ in range(2))
+    n = 2 * page + 100
+    length = torch.full((1, hkv), n, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(1, hkv, d, generator=g, device="cuda").to(dt) for _ in range(3))
+    out = torch.empty_like(q)
+    c = B.D2OPagedCache(kp, vp, table, length, n_q_heads=hkv)
+    c.d2o_paged_decode_step(q, k, v, out)
+    K, V = (pool[table[0].long()].transpose(0, 1).flatten(1, 2)[:, :n + 1].double() for pool in (kp, vp))
+    assert torch.equal(K[:, n], k[0].double()) and torch.equal(V[:, n], v[0].double())
+    p = torch.softmax(torch.einsum("hd,hnd->hn", q[0].double(), K) / math.sqrt(d), -1)
+    torch.testing.assert_close(out[0].double(), torch.einsum("hn,hnd->hd", p, V), rtol=2.0 ** -8, atol=1e-5)
+    more = torch.randn(1, hkv, 5, d, generator=g, device="cuda").to(dt)
+    c.d2o_paged_append(more, more)
+    assert torch.equal(kp[n_pages - 3, :, 100:105], more[0]) and torch.equal(vp[n_pages - 3, :, 100:105], more[0])
+    c.check()
+
+
+# ---------------------------------------------------------------------------------------------- evict
+@pytest.mark.parametrize("b,hq,hkv,d,dtype,page,held,budget,window,sinks", [
+    (1, 1, 1, 64, "f32", 16, [1], [0], 0, 0), (1, 1, 1, 64, "f32", 16, [2], [1], 0, 0), (1, 2, 2, 128, "bf16", 16, [40], [39], 4, 1),
+    (2, 4, 2, 128, "f16", 16, [100, 33], [25, 32], 8, 2), (3, 4, 1, 64, "bf16", 32, [200, 5, 64], [64, 10, 64], 16, 4),
+    (2, 8, 8, 128, "f32", 64, [150, 151], [149, 3], 2, 1), (1, 4, 2, 64, "f16", 16, [700], [350], 0, 0), (2, 2, 2, 64, "bf16", 16, [-1, 90], [4, 80], 79, 1),
+    (1, 1, 1, 64, "f16", 128, [2100], [1], 0, 0), (1, 1, 1, 64, "bf16", 16, [600], [300], 1000, 0)])
+@pytest.mark.parametrize("kind", ["spread", "ties", "zeros", "special", "shuffled"])
+def test_evict(cuda_device, b, hq, hkv, d, dtype, page, held, budget, window, sinks, kind):
+    c = Paged(sum(held) + 1, b, hq, hkv, d, dtype, page, max(1, (max(held) + page - 1) // page), held)
+    s = c.score
+    if kind == "ties":
+        s.copy_(torch.where(s == s, (s * 4).floor(), s))
+    elif kind == "zeros":
+        s.copy_(torch.where(s == s, torch.where(s < 0.5, 0.0, -0.0), s))
+    elif kind == "special":
+        x = torch.rand(s.shape, generator=c.g)
+        s.copy_(torch.where(x < 0.1, NAN, torch.where(x < 0.2, -NAN, torch.where(x < 0.3, math.inf, torch.where(x < 0.5, -math.inf, torch.where(x < 0.6, -s, s))))))
+    elif kind == "shuffled":                                                   # positions in another order, with gaps
+        s.copy_(torch.where(s == s, (s * 8).floor(), s))
+        for i in range(b):
+            for h in range(hkv):
+                p = torch.randperm(2 * max(1, held[i]), generator=c.g)
+                for r in range(max(0, held[i])):
+                    pg, at = c.at(i, r)
+                    c.pos[pg, h, at] = int(p[r])
+    c.upload()
+    next_pos = torch.tensor([max(0, x) * (2 if kind == "shuffled" else 1) for x in held], dtype=torch.int32)
+    budgets = torch.tensor(budget, dtype=torch.int32)[:, None].expand(b, hkv).contiguous()
+    if hkv > 1:                                                                # heads with sizes of their own
+        budgets[:, 1] = (budgets[:, 1] - 1).clamp(min=0)
+    c.cache.d2o_paged_evict(budgets.cuda(), next_pos.cuda(), n_sink=sinks, window=window)
+    c.evict(budgets, next_pos, sinks, window)
+    c.same()
+    c.cache.check()
+
+
+@pytest.mark.parametrize("n,budget,b,hkv", [(30000, 6000, 1, 8), (30001, 29990, 1, 1), (20000, 3000, 40, 8)])
+def test_evict_long(cuda_device, n, budget, b, hkv):
+    """More rows than shared memory keeps keys of, ties at the border; checked on the GPU."""
+    page, d, dt = 64, 64, torch.float16
+    g = torch.Generator(device="cuda").manual_seed(n)
+    per = (n + page - 1) // page
+    table = torch.randperm(per * b + 1, generator=g, device="cuda")[: per * b].view(b, per).to(torch.int32)
+    shape = (per * b + 1, hkv, page)
+    pos = torch.zeros(shape, dtype=torch.int32, device="cuda")
+    slot = torch.arange(per * page, device="cuda").expand(b, hkv, -1)
+    flip = (n - 1 - slot).clamp(min=0).to(torch.int32)                         # positions against the order of the rows
+    pos[table.long()] = flip.view(b, hkv, per, page).transpose(1, 2)
+    score = (torch.rand(shape, generator=g, device="cuda") * 50).floor()
+    # a row's K and V name the row
+    kp = (torch.rand(*shape, 1, generator=g, device="cuda")).to(dt).expand(*shape, d).contiguous()
+    vp = (-kp).contiguous()
+    dense = lambda pool: pool[table.long()].transpose(1, 2).flatten(2, 3)
+    key = dense(score)[..., :n].double() * (1 << 20) - flip[..., :n].double()
+    key[..., n - 3:] += 1e15                                                   # positions 0 .. 2: sinks
+    want = torch.zeros(b, hkv, n, dtype=torch.bool, device="cuda").scatter_(-1, key.topk(budget).indices, True)
+    want_pos = dense(pos)[..., :n].clone()
+    for i in range(b):
+        for h in range(hkv):
+            to, frm = (~want[i, h, :budget]).nonzero()[:, 0], want[i, h, budget:].nonzero()[:, 0] + budget
+            want_pos[i, h, to] = want_pos[i, h, frm]
+    was = {p: dense(p_).clone() for p, p_ in (("k", kp), ("score", score))}
+    c = B.D2OPagedCache(kp, vp, table, torch.full((b, hkv), n, dtype=torch.int32, device="cuda"), n_q_heads=hkv, pos=pos, score=score)
+    c.d2o_paged_evict(torch.full((b, hkv), budget, dtype=torch.int32, device="cuda"), torch.full((b,), n, dtype=torch.int32, device="cuda"), n_sink=3)
+    got = dense(pos)[..., :n]
+    assert torch.equal(got, want_pos)
+    src = (n - 1 - got).long()                                                 # the row that each row's contents came from
+    assert torch.equal(dense(score)[..., :n], was["score"].gather(-1, src))
+    assert torch.equal(dense(kp)[..., :n, 3], was["k"][..., 3].gather(-1, src)) and torch.equal(dense(vp)[..., :n, :], -dense(kp)[..., :n, :])
+    c.check()
+
+
+# ---------------------------------------------------------------------------------------------- anomalies
+def test_bad_tables(cuda_device):
+    """Page numbers out of range and tables that are too short: reported, nothing read or written through them; other sequences go on."""
+    def fresh():
+        c = Paged(4, 3, 4, 2, 64, "bf16", 16, 3, [40, 40, 47])
+        c.table[1, 1] = 99
+        return c
+    up = lambda t: t.cuda()
+    c = fresh()
+    c.upload()
+    q, k, v = c.randn(3, 4, 64), c.randn(3, 2, 64), c.randn(3, 2, 64)
+    out = torch.full((3, 4, 64), 3.0, dtype=c.dt, device="cuda")
+    c.cache.d2o_paged_decode_step(up(q), up(k), up(v), out)
+    assert bool(out[1].isnan().all()) and bool(torch.isfinite(out[0].float()).all()) and bool(torch.isfinite(out[2].float()).all())
+    with pytest.raises(B.D2OError) as e:
+        c.cache.check()
+    assert e.value.status == 4
+    c.cache.check()                                                            # the word has been taken
+    c = fresh()
+    c.table[1, 1] = -1
+    c.len[2] = 48                                                              # row 48 has no page
+    c.upload()
+    c.cache.d2o_paged_decode_step(up(q), up(k), up(v), out)
+    assert bool(out[1].isnan().all()) and bool(out[2].isnan().all()) and bool(torch.isfinite(out[0].float()).all())
+    with pytest.raises(B.D2OError):
+        c.cache.check()
+    # append: what has a page is written
+    c = fresh()
+    c.len[1] = 10
+    c.upload()
+    K, V = c.randn(3, 2, 9, 64), c.randn(3, 2, 9, 64)
+    c.cache.d2o_paged_append(up(K), up(V))
+    for h in range(2):
+        got = c.dk.cpu()
+        assert torch.equal(got[int(c.table[1, 0]), h, 10:], K[1, h, :6]) and torch.equal(got[int(c.table[2, 2]), h, 15], K[2, h, 0])
+        assert torch.equal(got[int(c.table[0, 2]), h, 8:], K[0, h, :8])
+    was, now = (c.k == c.k).all(-1), (c.dk.cpu() == c.dk.cpu()).all(-1)
+    assert int((now & ~was).sum()) == 2 * 1 + 2 * 8 and bool((was <= now).all())          # sequence 1 held 40 rows in the fixture
+    with pytest.raises(B.D2OError):
+        c.cache.check()
+    # evict: the slice stays as it was
+    c = fresh()
+    c.upload()
+    c.len[2] = 49
+    c.dlen.copy_(c.len)
+    budgets = torch.full((3, 2), 20, dtype=torch.int32)
+    c.cache.d2o_paged_evict(up(budgets), torch.full((3,), 40, dtype=torch.int32, device="cuda"))
+    keep = c.len.clone()
+    c.len[1:] = -1
+    c.evict(budgets, torch.full((3,), 40), 0, 0)
+    c.len.copy_(keep)
+    c.same()
+    with pytest.raises(B.D2OError):
+        c.cache.check()
+    c.upload()
+    c.cache.d2o_paged_evict(torch.full((3, 2), -1, dtype=torch.int32, device="cuda"), torch.full((3,), 40, dtype=torch.int32, device="cuda"))
+    with pytest.raises(B.D2OError):
+        c.cache.check()
+
+
+# ---------------------------------------------------------------------------------------------- together
+def test_serving_run(cuda_device):
+    """Prompt attention -> column sums -> pages -> decode steps and evictions in turn, from a captured graph and without one: the same
+    bits; every step against the plain statements."""
+    b, hq, hkv, d, n, page, budget = 2, 8, 2, 128, 150, 16, 96
+    lens = torch.tensor([150, 121], dtype=torch.int32)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    Q, K, V = (torch.randn(b, h, n, d, generator=g, device="cuda").to(torch.bfloat16) for h in (hq, hkv, hkv))
+    lse, out_p = torch.zeros(b, hq, n, device="cuda"), torch.zeros_like(Q)
+    B.d2o_prompt_attention(Q, K, V, out_p, lse=lse, lens=lens.cuda())
+    ctx = B.D2OContext(B.make_config(n_layers=1, batch=b, n_q_heads=hq, n_kv_heads=hkv, d_head=d, dtype="bf16", prompt_len=n,
+                                     max_new_tokens=1, rho=0.5))
+    ctx.d2o_set_prompt_lens(lens)
+    ctx.d2o_layer_stats(0, Q, K, lse)
+    colsum = ctx.colsum(0).clone()
+    runs = []
+    for graph in (False, True):
+        c = Paged(5, b, hq, hkv, d, "bf16", page, 12, [0, 0])
+        c.cache.d2o_paged_append(K, V, lens=lens.cuda(), colsum=colsum)
+        c.append(K.cpu(), V.cpu(), lens, None, colsum.cpu())
+        c.same()
+        c.len += lens[:, None]
+        c.dlen.copy_(c.len)
+        seen = lens.clone()
+        dseen, budgets = seen.cuda(), torch.full((b, hkv), budget, dtype=torch.int32, device="cuda")
+        q, k, v = (torch.zeros(b, h, d, dtype=torch.bfloat16, device="cuda") for h in (hq, hkv, hkv))
+        out, g0, outs = torch.zeros_like(q), None, []
+
+        def token():
+            c.cache.d2o_paged_decode_step(q, k, v, out, positions=dseen)
+            c.dlen.add_(1)
+            dseen.add_(1)
+            c.cache.d2o_paged_evict(budgets, dseen, n_sink=1, window=24)
+            c.dlen.copy_(torch.minimum(c.dlen, budgets))
+        for step in range(5):
+            for x, h in ((q, hq), (k, hkv), (v, hkv)):
+                x.copy_(c.randn(b, h, d))
+            if graph and step == 0:
+                keep = [t.clone() for t in (c.dk, c.dv, c.dpos, c.dscore, c.dlen, dseen)]
+                s = torch.cuda.Stream()
+                s.wait_stream(torch.cuda.current_stream())
+                with torch.cuda.stream(s):
+                    token()                                                    # once outside of the capture
+                torch.cuda.current_stream().wait_stream(s)
+                for t, was in zip((c.dk, c.dv, c.dpos, c.dscore, c.dlen, dseen), keep):
+                    t.copy_(was)
+                g0 = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(g0):
+                    token()
+            g0.replay() if graph else token()
+            torch.cuda.synchronize()
+            outs.append(out.clone())
+            if not graph:
+                dk = [t.clone() for t in (c.dk, c.dv, c.dpos, c.dscore)]
+                # the scores moved with the rows: compare the step by itself on a second cache
+                two = Paged(5, b, hq, hkv, d, "bf16", page, 12, [0, 0])
+                two.k, two.v, two.pos, two.score, two.len, two.table = c.k, c.v, c.pos, c.score, c.len, c.table
+                two.upload()
+                two.cache.d2o_paged_decode_step(q, k, v, out, positions=seen.cuda())
+                two.step(q.cpu(), k.cpu(), v.cpu(), out, seen, 0, 0)
+                two.same()
+                c.len += 1
+                seen = seen + 1
+                c.evict(budgets.cpu(), seen, 1, 24)
+                c.len.clamp_(max=budget)
+                assert all(np.array_equal(bits(x), bits(y)) for x, y in zip(dk, (c.k, c.v, c.pos, c.score)))
+                c.same()
+                assert torch.equal(dseen.cpu(), seen)
+        c.cache.check()
+        runs.append((outs, [bits(t) for t in (c.dk, c.dv, c.dpos, c.dscore)]))
+    assert all(torch.equal(x, y) for x, y in zip(runs[0][0], runs[1][0]))
+    assert all(np.array_equal(x, y) for x, y in zip(runs[0][1], runs[1][1]))
+    ctx.close()

@@ -1,0 +1,158 @@
+"""d2o_prompt_attention against float64: lengths around its tiles, windows and sinks, ragged batches with anything in the padding,
+grouped heads, both uses of its normalisers.
+
+Tolerance.  A logit is a sum of d products in fp32; its error is a few 2^-24 of the magnitudes that it sums, at most
+delta = 16 * 2^-24 * max_ij sum_e |q_ie k_je| / sqrt(d) (sixteen: partial sums of up to 16 elements at a time, four levels, and the
+scale).  A weight is then off by a factor of at most 1 + 2 delta (itself and the sum), plus the rounding of exp2 and of the sum
+(2^-21).  16-bit inputs: each weight is rounded once more for its product, by half a step.  So an output before its own rounding is
+within e = (half a step of the weights' type + 2 delta + 2^-21) * sum_j p_ij |v_j| of the reference, and the result must be the
+rounding of something in that interval.  lse is off by delta, and by the rounding of itself and of a logarithm (2^-22 of
+max(1, |lse|))."""
+import math
+
+import pytest
+import torch
+
+from paper_2406_13035_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def reference(q, k, v, window, n_sink):
+    """One head in float64: (out, lse, sum p |v|, sum |q||k| / sqrt d at most)."""
+    q, k, v = q.double(), k.double(), v.double()
+    n, d = q.shape
+    i, j = torch.arange(n, device=q.device)[:, None], torch.arange(n, device=q.device)[None]
+    seen = (j <= i) & ((j > i - window) | (j < n_sink)) if window > 0 else j <= i
+    x = (q @ k.T / math.sqrt(d)).masked_fill(~seen, -math.inf)
+    lse = torch.logsumexp(x, 1)
+    p = torch.exp(x - lse[:, None])
+    return p @ v, lse, p @ v.abs(), float((q.abs() @ k.abs().T).max()) / math.sqrt(d)
+
+
+def check(q, k, v, out, lse, window, n_sink, dtype):
+    ref, ref_lse, mag, dots = reference(q, k, v, window, n_sink)
+    delta = 16 * 2.0 ** -24 * dots
+    weights = 0.0 if dtype == "f32" else torch.finfo(DT[dtype]).eps / 2
+    e = (weights + 2 * delta + 2.0 ** -21) * mag
+    lo, hi, got = (ref - e).to(DT[dtype]).double(), (ref + e).to(DT[dtype]).double(), out.double()
+    assert bool(((lo <= got) & (got <= hi)).all()), float(((got - ref).abs() / (e + ref.abs() * torch.finfo(DT[dtype]).eps)).max())
+    if lse is not None:
+        assert bool(((lse.double() - ref_lse).abs() <= delta + 2.0 ** -22 * ref_lse.abs().clamp(min=1)).all())
+
+
+def draw(seed, b, hq, hkv, n, d, dtype, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    r = lambda h: torch.randn(b, h, n, d, generator=g, device="cuda")
+    return (r(hq) * scale).to(DT[dtype]), r(hkv).to(DT[dtype]), r(hkv).to(DT[dtype])
+
+
+CASES = [  # batch, q heads, kv heads, d, tokens, window, sinks
+    (1, 1, 1, 64, 1, 0, 0), (1, 2, 1, 128, 2, 1, 0), (2, 2, 2, 64, 63, 0, 0), (1, 4, 1, 128, 64, 16, 4), (1, 8, 1, 64, 65, 1, 1),
+    (1, 3, 1, 128, 127, 64, 0), (1, 4, 4, 128, 128, 0, 0), (2, 4, 2, 64, 129, 128, 2), (1, 2, 2, 128, 255, 129, 130),
+    (1, 2, 1, 128, 256, 0, 0), (1, 2, 1, 128, 257, 100, 0), (1, 2, 2, 64, 300, 1000, 4), (1, 8, 2, 128, 513, 77, 5),
+    (1, 2, 2, 128, 700, 130, 300), (2, 4, 1, 64, 1000, 256, 1), (1, 4, 1, 128, 1153, 0, 0), (1, 2, 1, 128, 1500, 513, 129),
+    (40, 8, 8, 64, 70, 0, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("b,hq,hkv,d,n,window,sinks", CASES)
+def test_attention(cuda_device, b, hq, hkv, d, n, window, sinks, dtype):
+    q, k, v = draw(n + window, b, hq, hkv, n, d, dtype)
+    out, lse = torch.full_like(q, float("nan")), torch.full((b, hq, n), float("nan"), device="cuda")
+    status = torch.zeros(2, dtype=torch.int32, device="cuda")
+    B.d2o_prompt_attention(q, k, v, out, lse=lse, window=window, n_sink=sinks, status=status)
+    for i in range(0, b, 13):
+        for h in range(hq):
+            check(q[i, h], k[i, h * hkv // hq], v[i, h * hkv // hq], out[i, h], lse[i, h], window, sinks, dtype)
+    assert status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lens,window,sinks", [([0, 1, 200, 128], 0, 0), ([257, 300, 5, 131], 70, 3), ([129, 64, 300, 0], 0, 0), ([-4, 999, 1, 250], 33, 0)])
+def test_ragged(cuda_device, lens, window, sinks, dtype):
+    """Padding holds NaN and infinities, in all three inputs; the rows of the outputs there stay as they were.  No lse."""
+    n, d = 300, 128
+    q, k, v = draw(n, 4, 4, 2, n, d, dtype)
+    ends = [min(max(x, 0), n) for x in lens]
+    for i, m in enumerate(ends):
+        for t in (q, k, v):
+            t[i, :, m:] = float("inf" if i % 2 else "nan")
+    out = torch.full_like(q, 7.0)
+    B.d2o_prompt_attention(q, k, v, out, window=window, n_sink=sinks, lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    for i, m in enumerate(ends):
+        assert bool((out[i, :, m:] == 7).all())
+        for h in range(4 if m else 0):
+            check(q[i, h, :m], k[i, h // 2, :m], v[i, h // 2, :m], out[i, h, :m], None, window, sinks, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_large_logits(cuda_device, dtype):
+    """Logits in the hundreds that grow along the row, so that the running maximum moves in every tile, and fall, so that it never
+    does: the weights of all but a few keys underflow."""
+    n, d = 400, 64
+    for sign in (1, -1):
+        q, k, v = draw(5, 1, 1, 1, n, d, dtype)
+        k = (k * 0.05 + sign * torch.arange(n, device="cuda")[:, None] * 0.02).to(DT[dtype])
+        q = (q * 0.05 + 1.0).to(DT[dtype])
+        out, lse = torch.empty_like(q), torch.empty(1, 1, n, device="cuda")
+        B.d2o_prompt_attention(q, k, v, out, lse=lse)
+        check(q[0, 0], k[0, 0], v[0, 0], out[0, 0], lse[0, 0], 0, 0, dtype)
+
+
+def test_not_finite(cuda_device):
+    """A NaN key reaches the rows that see it and no others; +inf and -inf logits give NaN and 0 as the formula does."""
+    for dtype in DT:
+        q, k, v = draw(9, 1, 1, 1, 600, 64, dtype)
+        q[0, 0, :, 0] = 1.0
+        k[0, 0, :, 0] = 0.0
+        k[0, 0, 300, 0], k[0, 0, 500, 0] = float("-inf"), float("nan")
+        out, lse = torch.empty_like(q), torch.empty(1, 1, 600, device="cuda")
+        B.d2o_prompt_attention(q, k, v, out, lse=lse)
+        assert bool(torch.isfinite(out[0, 0, :500].float()).all()) and bool(out[0, 0, 500:].isnan().all()) and bool(lse[0, 0, 500:].isnan().all())
+        keep = torch.tensor([j for j in range(500) if j != 300], device="cuda")
+        # rows behind 300 are those of a prompt without that key
+        ref, ref_lse, _, _ = reference(q[0, 0][keep], k[0, 0][keep], v[0, 0][keep], 0, 0)
+        assert float((lse[0, 0][keep].double() - ref_lse).abs().max()) < 2e-5
+        k[0, 0, 500, 0] = float("inf")
+        B.d2o_prompt_attention(q, k, v, out, lse=lse)
+        assert bool(torch.isfinite(out[0, 0, :500].float()).all()) and bool(out[0, 0, 500:].isnan().all())
+
+
+def test_normalisers_feed_the_column_sums(cuda_device):
+    """lse as d2o_layer_stats takes it: the same column sums, to rounding, as with its own first sweep."""
+    q, k, v = draw(3, 1, 8, 2, 777, 128, "bf16")
+    sums = []
+    for given in (False, True):
+        ctx = B.D2OContext(B.make_config(n_layers=1, batch=1, n_q_heads=8, n_kv_heads=2, d_head=128, dtype="bf16", prompt_len=777,
+                                         max_new_tokens=1, rho=0.5))
+        lse, out = torch.empty(1, 8, 777, device="cuda"), torch.empty_like(q)
+        if given:
+            B.d2o_prompt_attention(q, k, v, out, lse=lse)
+        ctx.d2o_layer_stats(0, q, k, lse if given else None)
+        sums.append(ctx.colsum(0).clone())
+        ctx.close()
+    torch.testing.assert_close(sums[0], sums[1], rtol=2e-5, atol=1e-7)
+
+
+def test_streams_graph_and_repeats(cuda_device):
+    """On a stream other than the default one, captured and replayed with other inputs, the same bits every time."""
+    q, k, v = draw(11, 2, 4, 2, 385, 128, "f16")
+    want = torch.empty_like(q)
+    B.d2o_prompt_attention(q, k, v, want, window=100, n_sink=2)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    out, q2 = torch.zeros_like(q), torch.zeros_like(q)
+    with torch.cuda.stream(s):
+        B.d2o_prompt_attention(q2, k, v, out, window=100, n_sink=2)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        B.d2o_prompt_attention(q2, k, v, out, window=100, n_sink=2)
+    for _ in range(3):
+        q2.copy_(q)
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
