@@ -158,8 +158,7 @@ static cudaError_t launch_one(const PromptAttentionArgs& a, cudaStream_t st) {
 
 cudaError_t launch_prompt_attention(int dtype, int D, const PromptAttentionArgs& a, cudaStream_t st) {
   if (dtype == D2O_F32) return D == 64 ? launch_one<float, 64>(a, st) : launch_one<float, 128>(a, st);
-  if (dtype == D2O_F16) return D == 64 ? launch_one<__half, 64>(a, st) : launch_one<__half, 128>(a, st);
-  return D == 64 ? launch_one<__nv_bfloat16, 64>(a, st) : launch_one<__nv_bfloat16, 128>(a, st);
+  return launch_prompt_attention_tc(dtype, D, a, st);
 }
 
 }  // namespace d2o

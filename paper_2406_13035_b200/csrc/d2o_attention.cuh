@@ -41,5 +41,6 @@ struct PromptSpan {
 };
 
 cudaError_t launch_prompt_attention(int dtype, int D, const PromptAttentionArgs& a, cudaStream_t st);
+cudaError_t launch_prompt_attention_tc(int dtype, int D, const PromptAttentionArgs& a, cudaStream_t st);      // fp16, bf16
 
 }  // namespace d2o

@@ -1,0 +1,360 @@
+// Attention of a prompt (Eq. 2-3 over all positions at once), causal, over a window and the first tokens: 16-bit inputs on the
+// 5th-generation tensor cores.
+//
+// One item = 256 queries of a head, as two tiles of 128; keys and values stream in tiles of 128.  Per tile of keys and tile of
+// queries: S = Q K^T (128 x 128 x d) into tensor memory; a thread of the softmax warps owns one query = one tensor-memory lane,
+// so that maximum and sum run over its registers; the weights go back, rounded to 16 bits, into the columns that held S, from
+// where they are the A operand of O += P V (128 x d x 128, V read as it lies, MN-major).  The two query tiles take turns: while
+// one's weights are formed the tensor cores work for the other.
+//   warps 0-3, 4-7  softmax of the first / second query tile, and its output at the end
+//   warp 8          TMA producer: Q once per item, K and V through one ring (128-byte swizzle)
+//   warp 9          tensor-memory allocation, MMA issue
+// The weights are 2^(c s - m) with a reference m per query that moves only when the maximum has grown by more than 8 (in the log2
+// domain): O in tensor memory is then rescaled by the softmax warps themselves.  The product before it has finished by then: the
+// commit that announces a new S covers every product issued ahead of it.
+//
+// Rounding: weights to the input type for their product (relative half step 2^-9 bf16, 2^-12 fp16; the largest is 2^0 to 2^8, and
+// the errors of many keys average out); their sum and lse from the unrounded ones; S, O and all sums are fp32.
+#include <math.h>
+
+#include <algorithm>
+
+#include <cuda/std/type_traits>
+
+#include "d2o_attention.cuh"
+#include "d2o_common.cuh"
+#include "d2o_tc.cuh"
+
+namespace d2o {
+
+constexpr int kPaTile = 128;
+constexpr int kPaSoftWarps = 8;
+constexpr int kPaThreads = (kPaSoftWarps + 2) * 32;
+constexpr float kPaSlack = 8.f;              // growth of the maximum (log2 domain) that the reference leaves standing
+
+__host__ __device__ constexpr int pa_stages(int D) { return D == 128 ? 4 : 8; }
+
+struct PaMaps { CUtensorMap q, k, v; };
+
+// One item: 256 queries of one (sequence, head).  The last queries see the most keys: items are numbered with those of all heads
+// first, neighbouring heads (which share keys and values) next to one another.
+struct PaItem {
+  int bh, b, P, q0;
+  __device__ __forceinline__ PaItem(const PromptAttentionArgs& a, int i) {
+    const int heads = a.B * a.Hq, blocks = (a.P + 2 * kPaTile - 1) / (2 * kPaTile);
+    bh = i % heads; b = bh / a.Hq;
+    P = a.length(b);
+    q0 = (blocks - 1 - i / heads) * 2 * kPaTile;
+  }
+  __device__ __forceinline__ bool empty() const { return q0 >= P; }
+  __device__ __forceinline__ bool exists(int t) const { return q0 + t * kPaTile < P; }
+};
+
+// Does query tile t (first query w) see anything of the key tile at k0?
+__device__ __forceinline__ bool pa_valid(const PromptAttentionArgs& a, int w, int P, int k0) {
+  return w < P && k0 <= w && (k0 + kPaTile - 1 > w - a.window || k0 < a.n_sink);
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(kPaThreads, 1)
+prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps maps, int n_items) {
+  constexpr int KB = D / 64, BLOCK = kPaTile * 128, TILE = KB * BLOCK, STAGES = pa_stages(D);
+  constexpr uint32_t IDESC_QK = make_idesc(FMT, kPaTile, kPaTile), IDESC_PV = make_idesc(FMT, kPaTile, D) | kIdescBMn;
+  using T = typename cuda::std::conditional<FMT == 0, __half, __nv_bfloat16>::type;
+  const float c = (D == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
+
+  extern __shared__ __align__(1024) unsigned char pa_smem[];
+  unsigned char* sQ = pa_smem;                               // [2 tiles][KB][128 rows][128 B]
+  unsigned char* sKV = pa_smem + 2 * TILE;                   // [stages][KB][128 rows][128 B]
+  __shared__ unsigned long long q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2], o_full[2], o_empty[2], all_done;
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_fail;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  if (tid == 0) {
+    s_fail = (tc::smem_u32(pa_smem) & 1023u) != 0u;          // swizzled tiles need 1024-byte aligned shared memory
+    tc::mbar_init(&q_full, 1); tc::mbar_init(&q_empty, 1); tc::mbar_init(&all_done, 1);
+    for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&kv_full[s], 1); tc::mbar_init(&kv_empty[s], 1); }
+    for (int t = 0; t < 2; ++t) { tc::mbar_init(&s_full[t], 1); tc::mbar_init(&p_ready[t], 4); tc::mbar_init(&o_full[t], 1); tc::mbar_init(&o_empty[t], 4); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == kPaSoftWarps + 1) {
+    tc::tmem_alloc(&s_tmem, 512);
+    tc::tmem_relinquish();
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tm_s = s_tmem, tm_o = s_tmem + 256;         // S (and P) of tile t at + 128 t, O at + 128 t
+  auto wait = [&](unsigned long long* bar, uint32_t parity) {
+    if (!s_fail && tc::mbar_wait(bar, parity)) return true;
+    s_fail = 1;
+    return false;
+  };
+  start_dependents();
+  wait_for_prior_grid();
+  int loads_q = 0, loads_kv = 0;                             // of the producer
+
+  if (warp == kPaSoftWarps) {
+    // ======================================================================= TMA producer
+    if (lane == 0) {
+      for (int i = blockIdx.x; i < n_items && !s_fail; i += gridDim.x) {
+        const PaItem it(a, i);
+        if (it.empty()) continue;
+        const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
+        const int q_row = it.bh * a.P + it.q0, k_base = (it.b * a.Hkv + it.bh % a.Hq / (a.Hq / a.Hkv)) * a.P;
+        for (int j = 0; j < 2 * span.tiles; ++j) {           // K, V, K, V ..
+          const int s = loads_kv % STAGES;
+          if (loads_kv >= STAGES && !wait(&kv_empty[s], (uint32_t)((loads_kv / STAGES - 1) & 1))) break;
+          tc::mbar_expect_tx(&kv_full[s], TILE);
+          for (int kb = 0; kb < KB; ++kb)
+            tc::tma_load_2d(sKV + s * TILE + kb * BLOCK, j & 1 ? &maps.v : &maps.k, kb * 64, k_base + span.tile(j >> 1) * kPaTile, &kv_full[s]);
+          ++loads_kv;
+          if (j == 0) {
+            if (loads_q >= 1 && !wait(&q_empty, (uint32_t)((loads_q - 1) & 1))) break;
+            tc::mbar_expect_tx(&q_full, 2 * TILE);
+            for (int t = 0; t < 2; ++t)
+              for (int kb = 0; kb < KB; ++kb) tc::tma_load_2d(sQ + t * TILE + kb * BLOCK, &maps.q, kb * 64, q_row + t * kPaTile, &q_full);
+            ++loads_q;
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == kPaSoftWarps + 1) {
+    // ======================================================================= MMA issue (the whole warp walks, lane 0 issues)
+    int ring = 0, items = 0;
+    int np[2] = {0, 0}, no[2] = {0, 0};                      // weights taken, items begun, per query tile
+    for (int i = blockIdx.x; i < n_items && !s_fail; i += gridDim.x) {
+      const PaItem it(a, i);
+      if (it.empty()) continue;
+      const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
+      const int n = span.tiles;
+      auto valid = [&](int t, int j) { return pa_valid(a, it.q0 + t * kPaTile, it.P, span.tile(j) * kPaTile); };
+      auto qk = [&](int t, int s) {
+        if (lane == 0) {
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) {
+            const uint64_t ad = tc::smem_desc_sw128(tc::smem_u32(sQ + t * TILE + kb * BLOCK)), bd = tc::smem_desc_sw128(tc::smem_u32(sKV + s * TILE + kb * BLOCK));
+#pragma unroll
+            for (int k = 0; k < 4; ++k)                      // 16 elements = 32 bytes along d per instruction
+              tc::mma_f16(tm_s + t * 128, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), IDESC_QK, (kb | k) != 0 ? 1u : 0u);
+          }
+          tc::mma_commit(&s_full[t]);
+        }
+      };
+      bool begun[2] = {false, false};
+      if (!wait(&q_full, (uint32_t)(items & 1)) || !wait(&kv_full[ring % STAGES], (uint32_t)((ring / STAGES) & 1))) break;
+      ++items;
+      tc::fence_after_sync();
+      for (int t = 0; t < 2; ++t)
+        if (valid(t, 0)) qk(t, ring % STAGES);
+      if (lane == 0) { tc::mma_commit(&kv_empty[ring % STAGES]); if (n == 1) tc::mma_commit(&q_empty); }
+      ++ring;
+      for (int j = 0; j < n; ++j) {
+        const int sv = ring % STAGES, sk = (ring + 1) % STAGES;
+        if (!wait(&kv_full[sv], (uint32_t)((ring / STAGES) & 1))) break;
+        const int k0 = span.tile(j) * kPaTile;
+        if (k0 + kPaTile > it.P) {
+          // values behind the sequence's end may be anything, and 0 * NaN is NaN: zero them
+          for (int x = lane; x < (k0 + kPaTile - it.P) * KB * 8; x += 32) {
+            const int r = it.P - k0 + x / (KB * 8), piece = x % (KB * 8);
+            *reinterpret_cast<uint4*>(sKV + sv * TILE + piece / 8 * BLOCK + r * 128 + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        bool next_k = false;
+        auto need_k = [&]() {
+          if (!next_k) { next_k = true; (void)wait(&kv_full[sk], (uint32_t)(((ring + 1) / STAGES) & 1)); }
+        };
+        for (int t = 0; t < 2 && !s_fail; ++t) {
+          if (valid(t, j)) {
+            if (!wait(&p_ready[t], (uint32_t)(np[t]++ & 1))) break;
+            if (!begun[t] && no[t]++ > 0 && !wait(&o_empty[t], (uint32_t)(no[t] & 1))) break;
+            tc::fence_after_sync();
+            if (lane == 0) {
+              const uint64_t bd = tc::smem_desc_sw128_mn(tc::smem_u32(sKV + sv * TILE), BLOCK);
+#pragma unroll
+              for (int k = 0; k < kPaTile / 16; ++k)         // 16 keys: 8 columns of weights, 16 rows of 128 bytes of V
+                tc::mma_f16_ts(tm_o + t * 128, tm_s + t * 128 + k * 8, bd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, begun[t] || k != 0 ? 1u : 0u);
+              if (k0 == it.q0 + t * kPaTile) tc::mma_commit(&o_full[t]);       // the diagonal: the tile's last keys
+            }
+            begun[t] = true;
+          }
+          // S again: its columns held the weights of the product just issued, and products run in the order of their issue
+          if (j + 1 < n && valid(t, j + 1)) {
+            need_k();
+            tc::fence_after_sync();
+            if (!s_fail) qk(t, sk);
+          }
+        }
+        if (j + 1 < n) need_k();
+        if (s_fail) break;
+        if (lane == 0) {
+          tc::mma_commit(&kv_empty[sv]);
+          if (j + 1 < n) tc::mma_commit(&kv_empty[sk]);
+          if (j + 2 == n) tc::mma_commit(&q_empty);          // the last product with Q has been issued
+        }
+        ring += j + 1 < n ? 2 : 1;
+      }
+    }
+    if (s_fail && lane == 0) {                               // tensor memory is freed behind the last products
+      tc::mma_commit(&all_done);
+      (void)tc::mbar_wait(&all_done, 0);
+    }
+    __syncwarp();
+  } else {
+    // ======================================================================= softmax, output
+    const int t = warp >> 2, quarter = warp & 3;             // query tile; tensor-memory lanes 32 * quarter ..
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t ts = tm_s + t * 128 + lanes, to = tm_o + t * 128 + lanes;
+    int ns = 0, items = 0;
+    for (int i = blockIdx.x; i < n_items && !s_fail; i += gridDim.x) {
+      const PaItem it(a, i);
+      if (it.empty() || !it.exists(t)) continue;
+      const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
+      const int w0 = it.q0 + t * kPaTile, r0 = w0 + quarter * 32, row = r0 + lane;      // first query of tile and warp, this thread's
+      float m = -INFINITY, l = 0.f;                          // reference (log2 domain), sum
+      for (int j = 0; j < span.tiles; ++j) {
+        const int k0 = span.tile(j) * kPaTile;
+        if (!pa_valid(a, w0, it.P, k0)) continue;
+        if (!__all_sync(0xffffffffu, wait(&s_full[t], (uint32_t)(ns++ & 1)))) break;
+        tc::fence_after_sync();
+        uint32_t s[4][32];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) tc::tmem_ld32_issue(ts + x * 32, s[x]);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) tc::tmem_ld_wait(s[x]);
+        // does the whole warp see the whole tile?
+        if (!(k0 + kPaTile - 1 <= r0 && (k0 > r0 + 31 - a.window || k0 + kPaTile <= a.n_sink))) {
+          const int last = row - k0, lo = row - a.window - k0, sink = a.n_sink - k0;    // seen: i <= last and (i > lo or i < sink)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const int i = x * 32 + e;
+              if (!(i <= last && (i > lo || i < sink))) s[x][e] = 0xff800000u;
+            }
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < 32; e += 2)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) mx[x] = tc::max3(mx[x], __uint_as_float(s[x][e]), __uint_as_float(s[x][e + 1]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        const bool first = m == -INFINITY;                   // nothing seen so far: O (if any) and l are zero
+        const bool move = !first && top > m + kPaSlack;
+        if (__any_sync(0xffffffffu, move)) {
+          const float f = move ? tc::ex2(m - top) : 1.f;
+          l *= f;
+#pragma unroll 1
+          for (int x = 0; x < D / 32; ++x) {
+            uint32_t o[32];
+            tc::tmem_ld32_issue(to + x * 32, o);
+            tc::tmem_ld_wait(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tc::tmem_st32(to + x * 32, o);
+          }
+        }
+        if (first || move) m = top;
+        const float b = m > -INFINITY ? -m : 0.f;
+        const tc::f32x2 c2 = tc::pack2(c, c), b2 = tc::pack2(b, b);
+        tc::f32x2 sum[2] = {0ull, 0ull};
+#pragma unroll
+        for (int x = 0; x < 4; x += 2) {
+          uint32_t p[32];
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            const uint32_t s0 = e < 32 ? s[x][e & 31] : s[x + 1][e & 31], s1 = e < 32 ? s[x][(e + 1) & 31] : s[x + 1][(e + 1) & 31];
+            const tc::f32x2 y = tc::fma2(tc::pack2(__uint_as_float(s0), __uint_as_float(s1)), c2, b2);
+            float y0, y1;
+            tc::unpack2(y, y0, y1);
+            y0 = tc::ex2(y0); y1 = tc::ex2(y1);
+            sum[(e >> 1) & 1] = tc::add2(sum[(e >> 1) & 1], tc::pack2(y0, y1));
+            if (FMT == 0) { const __half2 h = __floats2half2_rn(y0, y1); p[e / 2] = *reinterpret_cast<const uint32_t*>(&h); }
+            else { const __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1); p[e / 2] = *reinterpret_cast<const uint32_t*>(&h); }
+          }
+          tc::tmem_st32(ts + x * 16, p);
+        }
+        float lo, hi;
+        tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
+        l += lo + hi;
+        tc::tmem_st_wait();
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&p_ready[t]);
+      }
+      if (!__all_sync(0xffffffffu, wait(&o_full[t], (uint32_t)(items++ & 1)))) break;
+      tc::fence_after_sync();
+      const float f = 1.f / l;
+      T* out = (T*)a.out + ((size_t)it.bh * a.P + row) * D;
+#pragma unroll 1
+      for (int x = 0; x < D / 32; ++x) {
+        uint32_t o[32];
+        tc::tmem_ld32_issue(to + x * 32, o);
+        tc::tmem_ld_wait(o);
+        if (row < it.P) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            float y[8];
+#pragma unroll
+            for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * f;
+            *reinterpret_cast<uint4*>(out + x * 32 + e) = Elem<T>::pack(y);
+          }
+        }
+      }
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&o_empty[t]);
+      if (a.lse && row < it.P) a.lse[(size_t)it.bh * a.P + row] = (m + log2f(l)) * 0.6931471805599453f;
+    }
+  }
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == kPaSoftWarps + 1) {
+    tc::fence_after_sync();
+    tc::tmem_dealloc(s_tmem, 512);
+  }
+  if (s_fail) {
+    if (tid == kPaSoftWarps * 32) {                          // see the copies on their way land before the CTA may end
+      for (int i = max(0, loads_kv - STAGES); i < loads_kv; ++i)
+        if (!tc::mbar_wait(&kv_full[i % STAGES], (uint32_t)((i / STAGES) & 1))) break;
+      if (loads_q > 0) (void)tc::mbar_wait(&q_full, (uint32_t)((loads_q - 1) & 1));
+      if (a.status) report_error(a.status, D2O_ERR_TIMEOUT, 0xA7710000u | (uint32_t)(blockIdx.x & 0xffff));
+    }
+    for (int i = blockIdx.x; i < n_items; i += gridDim.x) {  // NaN for all items of this CTA
+      const PaItem it(a, i);
+      for (int r = it.q0 + tid; r < min(it.P, it.q0 + 2 * kPaTile); r += kPaThreads) {
+        for (int e = 0; e < D; ++e) ((T*)a.out)[((size_t)it.bh * a.P + r) * D + e] = Elem<T>::from_float(NAN);
+        if (a.lse) a.lse[(size_t)it.bh * a.P + r] = NAN;
+      }
+    }
+  }
+}
+
+template <int D, int FMT>
+static cudaError_t launch_one(const PromptAttentionArgs& a, const PaMaps& maps, cudaStream_t st) {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return cudaGetLastError();
+  const size_t smem = (size_t)(2 + pa_stages(D)) * (D / 64) * kPaTile * 128;
+  cudaError_t e = cudaFuncSetAttribute(prompt_attention_tc_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int n_items = a.B * a.Hq * ((a.P + 2 * kPaTile - 1) / (2 * kPaTile));
+  return launch_behind(prompt_attention_tc_kernel<D, FMT>, dim3((unsigned)std::min(n_items, sms)), kPaThreads, smem, st, a, maps, n_items);
+}
+
+cudaError_t launch_prompt_attention_tc(int dtype, int D, const PromptAttentionArgs& a, cudaStream_t st) {
+  PaMaps maps;
+  if (!encode_rows_2d(&maps.q, dtype, a.Q, (uint64_t)a.B * a.Hq * a.P, D, kPaTile) ||
+      !encode_rows_2d(&maps.k, dtype, a.K, (uint64_t)a.B * a.Hkv * a.P, D, kPaTile) ||
+      !encode_rows_2d(&maps.v, dtype, a.V, (uint64_t)a.B * a.Hkv * a.P, D, kPaTile))
+    return cudaErrorNotSupported;
+  if (dtype == D2O_F16) return D == 64 ? launch_one<64, 0>(a, maps, st) : launch_one<128, 0>(a, maps, st);
+  return D == 64 ? launch_one<64, 1>(a, maps, st) : launch_one<128, 1>(a, maps, st);
+}
+
+}  // namespace d2o
