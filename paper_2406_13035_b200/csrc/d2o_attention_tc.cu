@@ -8,7 +8,8 @@
 // one's weights are formed the tensor cores work for the other.
 //   warps 0-3, 4-7  softmax of the first / second query tile, and its output at the end
 //   warp 8          TMA producer: Q once per item, K and V through one ring (128-byte swizzle)
-//   warp 9          tensor-memory allocation, MMA issue
+//   warps 9, 10     MMA issue, one per query tile, in turns; the first allocates the tensor memory
+//   (warp 11 only completes its warpgroup)
 // The weights are 2^(c s - m) with a reference m per query that moves only when the maximum has grown by more than 8 (in the log2
 // domain): O in tensor memory is then rescaled by the softmax warps themselves.  The product before it has finished by then: the
 // commit that announces a new S covers every product issued ahead of it.
@@ -29,7 +30,7 @@ namespace d2o {
 
 constexpr int kPaTile = 128;
 constexpr int kPaSoftWarps = 8;
-constexpr int kPaThreads = (kPaSoftWarps + 2) * 32;
+constexpr int kPaThreads = (kPaSoftWarps + 4) * 32;          // three warpgroups: registers move between whole ones
 constexpr float kPaSlack = 8.f;              // growth of the maximum (log2 domain) that the reference leaves standing
 
 __host__ __device__ constexpr int pa_stages(int D) { return D == 128 ? 4 : 8; }
@@ -50,9 +51,46 @@ struct PaItem {
   __device__ __forceinline__ bool exists(int t) const { return q0 + t * kPaTile < P; }
 };
 
+// The x-th item of a CTA.  Items come heaviest first, so every second round goes through the CTAs backwards.
+__device__ __forceinline__ int pa_item(int x) {
+  const int c = (int)blockIdx.x, n = (int)gridDim.x;
+  return x * n + (x & 1 ? n - 1 - c : c);
+}
+
 // Does query tile t (first query w) see anything of the key tile at k0?
 __device__ __forceinline__ bool pa_valid(const PromptAttentionArgs& a, int w, int P, int k0) {
   return w < P && k0 <= w && (k0 + kPaTile - 1 > w - a.window || k0 < a.n_sink);
+}
+
+// 32 logits of a row: those not seen become -inf.  Column i is seen if i <= last and (i > low or i < sink).
+__device__ __forceinline__ void pa_mask(uint32_t (&s)[32], int last, int low, int sink) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    s[i] = (i <= last) & ((i > low) | (i < sink)) ? s[i] : 0xff800000u;       // no branches: with them 60 cycles per element
+}
+// 32 logits of a row: 2^(c s + b), in 16 bits in p[AT ..], and their sum.
+template <int FMT, int AT>
+__device__ __forceinline__ void pa_block(const uint32_t (&s)[32], uint32_t (&p)[32], float c, float b, tc::f32x2 (&sum)[2]) {
+  const tc::f32x2 c2 = tc::pack2(c, c), b2 = tc::pack2(b, b);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const tc::f32x2 y = tc::fma2(tc::pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), c2, b2);
+    float y0, y1;
+    tc::unpack2(y, y0, y1);
+    y0 = tc::ex2(y0); y1 = tc::ex2(y1);
+    sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(y0, y1));
+    if (FMT == 0) { const __half2 h = __floats2half2_rn(y0, y1); p[AT + i] = *reinterpret_cast<const uint32_t*>(&h); }
+    else { const __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1); p[AT + i] = *reinterpret_cast<const uint32_t*>(&h); }
+  }
+}
+
+// f(stage of `slot` as a constant): the descriptors are then constants too, where sums on the way to the uniform registers took
+// longer than the products.
+template <int STAGES, int S = 0, typename F>
+__device__ __forceinline__ void pa_each_stage(int slot, F&& f) {
+  if constexpr (S + 1 == STAGES) f(cuda::std::integral_constant<int, S>{});
+  else if (slot % STAGES == S) f(cuda::std::integral_constant<int, S>{});
+  else pa_each_stage<STAGES, S + 1>(slot, f);
 }
 
 template <int D, int FMT>
@@ -66,16 +104,16 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   extern __shared__ __align__(1024) unsigned char pa_smem[];
   unsigned char* sQ = pa_smem;                               // [2 tiles][KB][128 rows][128 B]
   unsigned char* sKV = pa_smem + 2 * TILE;                   // [stages][KB][128 rows][128 B]
-  __shared__ unsigned long long q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2], o_full[2], o_empty[2], all_done;
+  __shared__ unsigned long long q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2][2], o_full[2], o_empty[2], turn[2], all_done[2];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_fail;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
     s_fail = (tc::smem_u32(pa_smem) & 1023u) != 0u;          // swizzled tiles need 1024-byte aligned shared memory
-    tc::mbar_init(&q_full, 1); tc::mbar_init(&q_empty, 1); tc::mbar_init(&all_done, 1);
-    for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&kv_full[s], 1); tc::mbar_init(&kv_empty[s], 1); }
-    for (int t = 0; t < 2; ++t) { tc::mbar_init(&s_full[t], 1); tc::mbar_init(&p_ready[t], 4); tc::mbar_init(&o_full[t], 1); tc::mbar_init(&o_empty[t], 4); }
+    tc::mbar_init(&q_full, 1); tc::mbar_init(&q_empty, 2);
+    for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&kv_full[s], 1); tc::mbar_init(&kv_empty[s], 2); }
+    for (int t = 0; t < 2; ++t) { tc::mbar_init(&s_full[t], 1); tc::mbar_init(&p_ready[t][0], 4); tc::mbar_init(&p_ready[t][1], 4); tc::mbar_init(&o_full[t], 1); tc::mbar_init(&o_empty[t], 4); tc::mbar_init(&turn[t], 1); tc::mbar_init(&all_done[t], 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -88,6 +126,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   tc::fence_after_sync();
   const uint32_t tm_s = s_tmem, tm_o = s_tmem + 256;         // S (and P) of tile t at + 128 t, O at + 128 t
   auto wait = [&](unsigned long long* bar, uint32_t parity) {
+    if (tc::mbar_try_wait(bar, parity)) return true;
     if (!s_fail && tc::mbar_wait(bar, parity)) return true;
     s_fail = 1;
     return false;
@@ -96,10 +135,13 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   wait_for_prior_grid();
   int loads_q = 0, loads_kv = 0;                             // of the producer
 
-  if (warp == kPaSoftWarps) {
+  if (warp >= kPaSoftWarps) {
+    // 384 threads of 168 registers at launch: 256 of 208 and 128 of 88 from here on
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    if (warp == kPaSoftWarps) {
     // ======================================================================= TMA producer
     if (lane == 0) {
-      for (int i = blockIdx.x; i < n_items && !s_fail; i += gridDim.x) {
+      for (int x = 0, i; (i = pa_item(x)) < n_items && !s_fail; ++x) {
         const PaItem it(a, i);
         if (it.empty()) continue;
         const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
@@ -122,96 +164,93 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       }
     }
     __syncwarp();
-  } else if (warp == kPaSoftWarps + 1) {
-    // ======================================================================= MMA issue (the whole warp walks, lane 0 issues)
-    int ring = 0, items = 0;
-    int np[2] = {0, 0}, no[2] = {0, 0};                      // weights taken, items begun, per query tile
-    for (int i = blockIdx.x; i < n_items && !s_fail; i += gridDim.x) {
+  } else if (warp < kPaSoftWarps + 3) {
+    // ======================================================================= MMA issue: a warp per query tile
+    const int t = warp - kPaSoftWarps - 1;
+    const uint32_t ts = tm_s + t * 128, to = tm_o + t * 128;
+    int ring = 0, items = 0, turns = 0, np = 0, no = 0;      // tiles of keys or values, items, turns, weights taken, outputs begun
+    auto full = [&](int slot) { return wait(&kv_full[slot % STAGES], (uint32_t)((slot / STAGES) & 1)); };
+    for (int x = 0, i; (i = pa_item(x)) < n_items && !s_fail; ++x) {
       const PaItem it(a, i);
       if (it.empty()) continue;
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
-      const int n = span.tiles;
-      auto valid = [&](int t, int j) { return pa_valid(a, it.q0 + t * kPaTile, it.P, span.tile(j) * kPaTile); };
-      auto qk = [&](int t, int s) {
-        if (lane == 0) {
+      const int n = span.tiles, w0 = it.q0 + t * kPaTile;
+      auto qk = [&](int slot) {
+        const uint64_t q_desc = tc::smem_desc_sw128(tc::smem_u32(pa_smem + t * TILE));
+        pa_each_stage<STAGES>(slot, [&](auto stage) __attribute__((always_inline)) {
+          const uint64_t bd = tc::smem_desc_sw128(tc::smem_u32(pa_smem + (2 + decltype(stage)::value) * TILE));
 #pragma unroll
-          for (int kb = 0; kb < KB; ++kb) {
-            const uint64_t ad = tc::smem_desc_sw128(tc::smem_u32(sQ + t * TILE + kb * BLOCK)), bd = tc::smem_desc_sw128(tc::smem_u32(sKV + s * TILE + kb * BLOCK));
-#pragma unroll
-            for (int k = 0; k < 4; ++k)                      // 16 elements = 32 bytes along d per instruction
-              tc::mma_f16(tm_s + t * 128, ad + (uint64_t)(2 * k), bd + (uint64_t)(2 * k), IDESC_QK, (kb | k) != 0 ? 1u : 0u);
-          }
-          tc::mma_commit(&s_full[t]);
-        }
+          for (int k = 0; k < D / 16; ++k)                   // 16 elements = 32 bytes along d per instruction
+            tc::mma_f16_one(ts, q_desc + (uint64_t)(k / 4 * (BLOCK >> 4) + k % 4 * 2), bd + (uint64_t)(k / 4 * (BLOCK >> 4) + k % 4 * 2), IDESC_QK, k != 0 ? 1u : 0u);
+        });
+        tc::mma_commit_one(&s_full[t]);
       };
-      bool begun[2] = {false, false};
-      if (!wait(&q_full, (uint32_t)(items & 1)) || !wait(&kv_full[ring % STAGES], (uint32_t)((ring / STAGES) & 1))) break;
+      uint32_t begun = 0;
+      if (!wait(&q_full, (uint32_t)(items & 1)) || !full(ring)) break;
       ++items;
       tc::fence_after_sync();
-      for (int t = 0; t < 2; ++t)
-        if (valid(t, 0)) qk(t, ring % STAGES);
-      if (lane == 0) { tc::mma_commit(&kv_empty[ring % STAGES]); if (n == 1) tc::mma_commit(&q_empty); }
+      bool now = pa_valid(a, w0, it.P, span.tile(0) * kPaTile);      // does the tile see anything of job j?
+      if (now) qk(ring);
+      tc::mma_commit_one(&kv_empty[ring % STAGES]);
+      if (n == 1) tc::mma_commit_one(&q_empty);
       ++ring;
       for (int j = 0; j < n; ++j) {
-        const int sv = ring % STAGES, sk = (ring + 1) % STAGES;
-        if (!wait(&kv_full[sv], (uint32_t)((ring / STAGES) & 1))) break;
         const int k0 = span.tile(j) * kPaTile;
-        if (k0 + kPaTile > it.P) {
-          // values behind the sequence's end may be anything, and 0 * NaN is NaN: zero them
+        const bool next = j + 1 < n && pa_valid(a, w0, it.P, span.tile(j + 1) * kPaTile);
+        if (!full(ring)) break;
+        if (k0 + kPaTile > it.P && now) {
+          // values behind the sequence's end may be anything, and 0 * NaN is NaN: zero them (both warps may: the same zeros)
           for (int x = lane; x < (k0 + kPaTile - it.P) * KB * 8; x += 32) {
             const int r = it.P - k0 + x / (KB * 8), piece = x % (KB * 8);
-            *reinterpret_cast<uint4*>(sKV + sv * TILE + piece / 8 * BLOCK + r * 128 + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(sKV + ring % STAGES * TILE + piece / 8 * BLOCK + r * 128 + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
-        bool next_k = false;
-        auto need_k = [&]() {
-          if (!next_k) { next_k = true; (void)wait(&kv_full[sk], (uint32_t)(((ring + 1) / STAGES) & 1)); }
-        };
-        for (int t = 0; t < 2 && !s_fail; ++t) {
-          if (valid(t, j)) {
-            if (!wait(&p_ready[t], (uint32_t)(np[t]++ & 1))) break;
-            if (!begun[t] && no[t]++ > 0 && !wait(&o_empty[t], (uint32_t)(no[t] & 1))) break;
-            tc::fence_after_sync();
-            if (lane == 0) {
-              const uint64_t bd = tc::smem_desc_sw128_mn(tc::smem_u32(sKV + sv * TILE), BLOCK);
+        if (j + 1 < n && !full(ring + 1)) break;
+        if (now && !begun && no++ > 0 && !wait(&o_empty[t], (uint32_t)(no & 1))) break;
+        if (!wait(&turn[t], (uint32_t)((turns++ & 1) ^ (t ^ 1)))) break;
+        if (now) {
+          pa_each_stage<STAGES>(ring, [&](auto stage) __attribute__((always_inline)) {
+            const uint64_t bd = tc::smem_desc_sw128_mn(tc::smem_u32(pa_smem + (2 + decltype(stage)::value) * TILE), BLOCK);
 #pragma unroll
-              for (int k = 0; k < kPaTile / 16; ++k)         // 16 keys: 8 columns of weights, 16 rows of 128 bytes of V
-                tc::mma_f16_ts(tm_o + t * 128, tm_s + t * 128 + k * 8, bd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, begun[t] || k != 0 ? 1u : 0u);
-              if (k0 == it.q0 + t * kPaTile) tc::mma_commit(&o_full[t]);       // the diagonal: the tile's last keys
+            for (int h = 0; h < 2; ++h) {                    // the weights of 64 keys at a time
+              (void)wait(&p_ready[t][h], (uint32_t)(np & 1));
+              tc::fence_after_sync();
+#pragma unroll
+              for (int k = h * kPaTile / 32; k < (h + 1) * kPaTile / 32; ++k)    // 16 keys: 8 columns of weights, 16 rows of 128 bytes of V
+                tc::mma_f16_ts_one(to, ts + k * 8, bd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, k != 0 ? 1u : begun);
             }
-            begun[t] = true;
-          }
-          // S again: its columns held the weights of the product just issued, and products run in the order of their issue
-          if (j + 1 < n && valid(t, j + 1)) {
-            need_k();
-            tc::fence_after_sync();
-            if (!s_fail) qk(t, sk);
-          }
+          });
+          ++np;
+          begun = 1;
         }
-        if (j + 1 < n) need_k();
-        if (s_fail) break;
-        if (lane == 0) {
-          tc::mma_commit(&kv_empty[sv]);
-          if (j + 1 < n) tc::mma_commit(&kv_empty[sk]);
-          if (j + 2 == n) tc::mma_commit(&q_empty);          // the last product with Q has been issued
-        }
+        // S again: its columns held the weights of the product just issued, and the products of one thread run in the order of
+        // their issue
+        if (next) qk(ring + 1);
+        if (lane == 0) tc::mbar_arrive(&turn[t ^ 1]);
+        if (now && k0 == w0) tc::mma_commit_one(&o_full[t]);  // the diagonal: the tile's last keys
+        tc::mma_commit_one(&kv_empty[ring % STAGES]);
+        if (j + 1 < n) tc::mma_commit_one(&kv_empty[(ring + 1) % STAGES]);
+        if (j + 2 == n) tc::mma_commit_one(&q_empty);         // the last product with Q has been issued
         ring += j + 1 < n ? 2 : 1;
+        now = next;
       }
     }
     if (s_fail && lane == 0) {                               // tensor memory is freed behind the last products
-      tc::mma_commit(&all_done);
-      (void)tc::mbar_wait(&all_done, 0);
+      tc::mma_commit(&all_done[t]);
+      (void)tc::mbar_wait(&all_done[t], 0);
     }
     __syncwarp();
+  }
   } else {
     // ======================================================================= softmax, output
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int t = warp >> 2, quarter = warp & 3;             // query tile; tensor-memory lanes 32 * quarter ..
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t ts = tm_s + t * 128 + lanes, to = tm_o + t * 128 + lanes;
     int ns = 0, items = 0;
-    for (int i = blockIdx.x; i < n_items && !s_fail; i += gridDim.x) {
+    for (int x = 0, i; (i = pa_item(x)) < n_items && !s_fail; ++x) {
       const PaItem it(a, i);
       if (it.empty() || !it.exists(t)) continue;
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
@@ -222,93 +261,87 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         if (!pa_valid(a, w0, it.P, k0)) continue;
         if (!__all_sync(0xffffffffu, wait(&s_full[t], (uint32_t)(ns++ & 1)))) break;
         tc::fence_after_sync();
-        uint32_t s[4][32];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) tc::tmem_ld32_issue(ts + x * 32, s[x]);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) tc::tmem_ld_wait(s[x]);
+        uint32_t s0[32], s1[32], s2[32], s3[32];
+        tc::tmem_ld32_issue(ts, s0); tc::tmem_ld32_issue(ts + 32, s1);
+        tc::tmem_ld32_issue(ts + 64, s2); tc::tmem_ld32_issue(ts + 96, s3);
+        tc::tmem_ld_wait(s0); tc::tmem_ld_wait(s1); tc::tmem_ld_wait(s2); tc::tmem_ld_wait(s3);
         // does the whole warp see the whole tile?
         if (!(k0 + kPaTile - 1 <= r0 && (k0 > r0 + 31 - a.window || k0 + kPaTile <= a.n_sink))) {
-          const int last = row - k0, lo = row - a.window - k0, sink = a.n_sink - k0;    // seen: i <= last and (i > lo or i < sink)
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int i = x * 32 + e;
-              if (!(i <= last && (i > lo || i < sink))) s[x][e] = 0xff800000u;
-            }
+          const int last = row - k0, low = row - a.window - k0, sink = a.n_sink - k0;
+          pa_mask(s0, last, low, sink); pa_mask(s1, last - 32, low - 32, sink - 32);
+          pa_mask(s2, last - 64, low - 64, sink - 64); pa_mask(s3, last - 96, low - 96, sink - 96);
         }
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 0; e < 32; e += 2)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) mx[x] = tc::max3(mx[x], __uint_as_float(s[x][e]), __uint_as_float(s[x][e + 1]));
+        for (int e = 0; e < 32; e += 2) {
+          mx[0] = tc::max3(mx[0], __uint_as_float(s0[e]), __uint_as_float(s0[e + 1]));
+          mx[1] = tc::max3(mx[1], __uint_as_float(s1[e]), __uint_as_float(s1[e + 1]));
+          mx[2] = tc::max3(mx[2], __uint_as_float(s2[e]), __uint_as_float(s2[e + 1]));
+          mx[3] = tc::max3(mx[3], __uint_as_float(s3[e]), __uint_as_float(s3[e + 1]));
+        }
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-        const bool first = m == -INFINITY;                   // nothing seen so far: O (if any) and l are zero
-        const bool move = !first && top > m + kPaSlack;
+        const bool first = m == -INFINITY, move = !first && top > m + kPaSlack;       // first: O (if any) and l are zero
         if (__any_sync(0xffffffffu, move)) {
           const float f = move ? tc::ex2(m - top) : 1.f;
           l *= f;
 #pragma unroll 1
-          for (int x = 0; x < D / 32; ++x) {
-            uint32_t o[32];
-            tc::tmem_ld32_issue(to + x * 32, o);
+          for (int x = 0; x < D; x += 16) {
+            uint32_t o[16];
+            tc::tmem_ld16_issue(to + x, o);
             tc::tmem_ld_wait(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tc::tmem_st32(to + x * 32, o);
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tc::tmem_st16(to + x, o);
           }
         }
         if (first || move) m = top;
         const float b = m > -INFINITY ? -m : 0.f;
-        const tc::f32x2 c2 = tc::pack2(c, c), b2 = tc::pack2(b, b);
         tc::f32x2 sum[2] = {0ull, 0ull};
-#pragma unroll
-        for (int x = 0; x < 4; x += 2) {
+        {
           uint32_t p[32];
-#pragma unroll
-          for (int e = 0; e < 64; e += 2) {
-            const uint32_t s0 = e < 32 ? s[x][e & 31] : s[x + 1][e & 31], s1 = e < 32 ? s[x][(e + 1) & 31] : s[x + 1][(e + 1) & 31];
-            const tc::f32x2 y = tc::fma2(tc::pack2(__uint_as_float(s0), __uint_as_float(s1)), c2, b2);
-            float y0, y1;
-            tc::unpack2(y, y0, y1);
-            y0 = tc::ex2(y0); y1 = tc::ex2(y1);
-            sum[(e >> 1) & 1] = tc::add2(sum[(e >> 1) & 1], tc::pack2(y0, y1));
-            if (FMT == 0) { const __half2 h = __floats2half2_rn(y0, y1); p[e / 2] = *reinterpret_cast<const uint32_t*>(&h); }
-            else { const __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1); p[e / 2] = *reinterpret_cast<const uint32_t*>(&h); }
-          }
-          tc::tmem_st32(ts + x * 16, p);
+          pa_block<FMT, 0>(s0, p, c, b, sum);
+          pa_block<FMT, 16>(s1, p, c, b, sum);
+          tc::tmem_st32(ts, p);
         }
-        float lo, hi;
-        tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
-        l += lo + hi;
         tc::tmem_st_wait();
         tc::fence_before_sync();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(&p_ready[t]);
+        if (lane == 0) tc::mbar_arrive(&p_ready[t][0]);
+        {
+          uint32_t p[32];
+          pa_block<FMT, 0>(s2, p, c, b, sum);
+          pa_block<FMT, 16>(s3, p, c, b, sum);
+          tc::tmem_st32(ts + 32, p);
+        }
+        tc::tmem_st_wait();
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&p_ready[t][1]);
+        float lo, hi;
+        tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
+        l += lo + hi;
       }
       if (!__all_sync(0xffffffffu, wait(&o_full[t], (uint32_t)(items++ & 1)))) break;
       tc::fence_after_sync();
       const float f = 1.f / l;
       T* out = (T*)a.out + ((size_t)it.bh * a.P + row) * D;
-#pragma unroll 1
-      for (int x = 0; x < D / 32; ++x) {
-        uint32_t o[32];
-        tc::tmem_ld32_issue(to + x * 32, o);
-        tc::tmem_ld_wait(o);
-        if (row < it.P) {
+      uint32_t o[D / 32][32];
 #pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            float y[8];
+      for (int x = 0; x < D / 32; ++x) tc::tmem_ld32_issue(to + x * 32, o[x]);
 #pragma unroll
-            for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e + z]) * f;
-            *reinterpret_cast<uint4*>(out + x * 32 + e) = Elem<T>::pack(y);
-          }
-        }
-      }
+      for (int x = 0; x < D / 32; ++x) tc::tmem_ld_wait(o[x]);
       tc::fence_before_sync();
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&o_empty[t]);
+      if (row < it.P) {
+#pragma unroll
+        for (int e = 0; e < D; e += 8) {
+          float y[8];
+#pragma unroll
+          for (int z = 0; z < 8; ++z) y[z] = __uint_as_float(o[e / 32][e % 32 + z]) * f;
+          *reinterpret_cast<uint4*>(out + e) = Elem<T>::pack(y);
+        }
+      }
       if (a.lse && row < it.P) a.lse[(size_t)it.bh * a.P + row] = (m + log2f(l)) * 0.6931471805599453f;
     }
   }
@@ -325,7 +358,8 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       if (loads_q > 0) (void)tc::mbar_wait(&q_full, (uint32_t)((loads_q - 1) & 1));
       if (a.status) report_error(a.status, D2O_ERR_TIMEOUT, 0xA7710000u | (uint32_t)(blockIdx.x & 0xffff));
     }
-    for (int i = blockIdx.x; i < n_items; i += gridDim.x) {  // NaN for all items of this CTA
+    for (int x = 0, i; x * (int)gridDim.x < n_items; ++x) {   // NaN for all items of this CTA
+      if ((i = pa_item(x)) >= n_items) continue;
       const PaItem it(a, i);
       for (int r = it.q0 + tid; r < min(it.P, it.q0 + 2 * kPaTile); r += kPaThreads) {
         for (int e = 0; e < D; ++e) ((T*)a.out)[((size_t)it.bh * a.P + r) * D + e] = Elem<T>::from_float(NAN);
