@@ -84,15 +84,6 @@ __device__ __forceinline__ void pa_block(const uint32_t (&s)[32], uint32_t (&p)[
   }
 }
 
-// f(stage of `slot` as a constant): the descriptors are then constants too, where sums on the way to the uniform registers took
-// longer than the products.
-template <int STAGES, int S = 0, typename F>
-__device__ __forceinline__ void pa_each_stage(int slot, F&& f) {
-  if constexpr (S + 1 == STAGES) f(cuda::std::integral_constant<int, S>{});
-  else if (slot % STAGES == S) f(cuda::std::integral_constant<int, S>{});
-  else pa_each_stage<STAGES, S + 1>(slot, f);
-}
-
 template <int D, int FMT>
 __global__ void __launch_bounds__(kPaThreads, 1)
 prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps maps, int n_items) {
@@ -176,13 +167,10 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
       const int n = span.tiles, w0 = it.q0 + t * kPaTile;
       auto qk = [&](int slot) {
-        const uint64_t q_desc = tc::smem_desc_sw128(tc::smem_u32(pa_smem + t * TILE));
-        pa_each_stage<STAGES>(slot, [&](auto stage) __attribute__((always_inline)) {
-          const uint64_t bd = tc::smem_desc_sw128(tc::smem_u32(pa_smem + (2 + decltype(stage)::value) * TILE));
+        const uint64_t ad = tc::smem_desc_sw128(tc::smem_u32(sQ + t * TILE)), bd = tc::smem_desc_sw128(tc::smem_u32(sKV + slot % STAGES * TILE));
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k)                   // 16 elements = 32 bytes along d per instruction
-            tc::mma_f16_one(ts, q_desc + (uint64_t)(k / 4 * (BLOCK >> 4) + k % 4 * 2), bd + (uint64_t)(k / 4 * (BLOCK >> 4) + k % 4 * 2), IDESC_QK, k != 0 ? 1u : 0u);
-        });
+        for (int k = 0; k < D / 16; ++k)                     // 16 elements = 32 bytes along d per instruction
+          tc::mma_f16_one(ts, ad + (uint64_t)(k / 4 * (BLOCK >> 4) + k % 4 * 2), bd + (uint64_t)(k / 4 * (BLOCK >> 4) + k % 4 * 2), IDESC_QK, k != 0 ? 1u : 0u);
         tc::mma_commit_one(&s_full[t]);
       };
       uint32_t begun = 0;
@@ -211,17 +199,15 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         if (now && !begun && no++ > 0 && !wait(&o_empty[t], (uint32_t)(no & 1))) break;
         if (!wait(&turn[t], (uint32_t)((turns++ & 1) ^ (t ^ 1)))) break;
         if (now) {
-          pa_each_stage<STAGES>(ring, [&](auto stage) __attribute__((always_inline)) {
-            const uint64_t bd = tc::smem_desc_sw128_mn(tc::smem_u32(pa_smem + (2 + decltype(stage)::value) * TILE), BLOCK);
+          const uint64_t bd = tc::smem_desc_sw128_mn(tc::smem_u32(sKV + ring % STAGES * TILE), BLOCK);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {                    // the weights of 64 keys at a time
-              (void)wait(&p_ready[t][h], (uint32_t)(np & 1));
-              tc::fence_after_sync();
+          for (int h = 0; h < 2; ++h) {                      // the weights of 64 keys at a time
+            (void)wait(&p_ready[t][h], (uint32_t)(np & 1));
+            tc::fence_after_sync();
 #pragma unroll
-              for (int k = h * kPaTile / 32; k < (h + 1) * kPaTile / 32; ++k)    // 16 keys: 8 columns of weights, 16 rows of 128 bytes of V
-                tc::mma_f16_ts_one(to, ts + k * 8, bd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, k != 0 ? 1u : begun);
-            }
-          });
+            for (int k = h * kPaTile / 32; k < (h + 1) * kPaTile / 32; ++k)      // 16 keys: 8 columns of weights, 16 rows of 128 bytes of V
+              tc::mma_f16_ts_one(to, ts + k * 8, bd + (uint64_t)(k * (2048 >> 4)), IDESC_PV, k != 0 ? 1u : begun);
+          }
           ++np;
           begun = 1;
         }
