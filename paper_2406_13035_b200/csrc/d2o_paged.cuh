@@ -65,7 +65,7 @@ struct PagedScratch {
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
     desc = take((size_t)n_slices * 16);
     lse2 = take((size_t)n_slices * group * 4);
-    parts = take((size_t)kPagedCtas * 2 * group * (D + 2) * 4);
+    parts = take((size_t)kPagedCtas * 2 * group * (D + 4) * 4);
     rows = take(scored ? pool_rows * (size_t)(group > 2 ? group * 4 : 8) : 0);
     end = o;
   }
