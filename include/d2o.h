@@ -340,8 +340,10 @@ typedef struct {
 } d2o_paged_cache;
 
 /* Bytes of DEVICE scratch (256-byte aligned) that d2o_paged_decode_step and d2o_paged_evict need for this cache (only the
- * sizes and whether `score` is NULL count).  Contents need not be kept or cleared between calls; two calls whose work may
+ * sizes and whether `score` is NULL count).  Its first D2O_PAGED_ZERO_BYTES are zero before the first call (the caller clears them
+ * once) and again after every call, whatever cache it was for; the rest need not be kept or cleared.  Two calls whose work may
  * overlap on the GPU need a scratch each, also as parts of graphs. */
+#define D2O_PAGED_ZERO_BYTES (65536u * 4u)
 d2o_status d2o_paged_workspace_size(const d2o_paged_cache* cache, size_t* bytes);
 
 /* Puts the rows of a prompt, or of a turn, behind those held: row i of sequence b goes to row len[b, h] + i, for i < lens[b].

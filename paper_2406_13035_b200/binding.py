@@ -29,6 +29,7 @@ EXPORTS = [
     "d2o_prompt_attention", "d2o_paged_workspace_size", "d2o_paged_append", "d2o_paged_decode_step", "d2o_paged_evict",
 ]
 STATIC_LSE_FLOATS = 1 << 20      # D2O_STATIC_LSE_FLOATS of include/d2o.h
+PAGED_ZERO_BYTES = 65536 * 4     # D2O_PAGED_ZERO_BYTES
 
 
 class D2OConfig(C.Structure):
@@ -402,10 +403,10 @@ def _arg(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> Optional
     """The address of a tensor that has to be contiguous, of this shape and type and on this device (None: NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
-        raise D2OError(1, f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, got "
-                          f"{t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.shape == shape and t.dtype is dtype and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    raise D2OError(1, f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, got "
+                      f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def _call(device: torch.device, what: str, fn, *args):
@@ -462,14 +463,16 @@ class D2OPagedCache:
         n = C.c_size_t()
         _check(self.lib.d2o_paged_workspace_size(C.byref(self.cache), C.byref(n)), "d2o_paged_workspace_size")
         self.scratch = torch.empty(n.value + 256, dtype=torch.uint8, device=dev)
+        self.scratch[:PAGED_ZERO_BYTES + 256].zero_()
         self._scratch = ((self.scratch.data_ptr() + 255) // 256 * 256, n.value)
+        self._ref = C.byref(self.cache)
 
     def d2o_paged_append(self, K: torch.Tensor, V: torch.Tensor, *, lens: Optional[torch.Tensor] = None,
                          first_pos: Optional[torch.Tensor] = None, colsum: Optional[torch.Tensor] = None):
         b, hq, hkv, d = self.shape
         _need(K.dim() == 4, "K, V: [B, Hkv, n_rows, d]")
         n, dev, i32 = K.shape[2], self.device, torch.int32
-        _call(dev, "d2o_paged_append", self.lib.d2o_paged_append, C.byref(self.cache), n,
+        _call(dev, "d2o_paged_append", self.lib.d2o_paged_append, self._ref, n,
               _arg(K, "K", (b, hkv, n, d), self.dtype, dev), _arg(V, "V", (b, hkv, n, d), self.dtype, dev),
               _arg(lens, "lens", (b,), i32, dev), _arg(first_pos, "first_pos", (b,), i32, dev),
               _arg(colsum, "colsum", (b, hq, n), torch.float32, dev))
@@ -478,13 +481,13 @@ class D2OPagedCache:
                               positions: Optional[torch.Tensor] = None, window: int = 0, n_sink: int = 0):
         b, hq, hkv, d = self.shape
         dev, dt = self.device, self.dtype
-        _call(dev, "d2o_paged_decode_step", self.lib.d2o_paged_decode_step, C.byref(self.cache), window, n_sink,
+        _call(dev, "d2o_paged_decode_step", self.lib.d2o_paged_decode_step, self._ref, window, n_sink,
               _arg(q, "q", (b, hq, d), dt, dev), _arg(k, "k", (b, hkv, d), dt, dev), _arg(v, "v", (b, hkv, d), dt, dev),
               _arg(positions, "positions", (b,), torch.int32, dev), _arg(out, "out", (b, hq, d), dt, dev), *self._scratch)
 
     def d2o_paged_evict(self, budgets: torch.Tensor, next_pos: torch.Tensor, *, n_sink: int = 0, window: int = 0):
         b, _, hkv, _ = self.shape
-        _call(self.device, "d2o_paged_evict", self.lib.d2o_paged_evict, C.byref(self.cache),
+        _call(self.device, "d2o_paged_evict", self.lib.d2o_paged_evict, self._ref,
               _arg(budgets, "budgets", (b, hkv), torch.int32, self.device), _arg(next_pos, "next_pos", (b,), torch.int32, self.device),
               n_sink, window, *self._scratch)
 

@@ -56,14 +56,15 @@ cudaError_t launch_paged_decode(const PagedView& p, int dtype, int D, int window
 cudaError_t launch_paged_evict(const PagedView& p, int dtype, int D, const int32_t* budgets, const int32_t* next_pos, int n_sink,
                                int window, char* scratch, cudaStream_t st);
 
-// Layout of the scratch (bytes): what the decode step's kernels hand over, and per row of the pools the logits of its query
+// Layout of the scratch (bytes): counters that are zero between calls, first and always of the same size; what the decode step's CTAs
+// hand over; and per row of the pools the logits of its query
 // heads, or an entry of the eviction's lists.
 struct PagedScratch {
-  size_t desc, lse2, parts, rows, end;
+  size_t done, lse2, parts, rows, end;
   PagedScratch(int n_slices, int group, int D, size_t pool_rows, bool scored) {
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
-    desc = take((size_t)n_slices * 16);
+    done = take((size_t)D2O_PAGED_ZERO_BYTES);
     lse2 = take((size_t)n_slices * group * 4);
     parts = take((size_t)kPagedCtas * 2 * group * (D + 4) * 4);
     rows = take(scored ? pool_rows * (size_t)(group > 2 ? group * 4 : 8) : 0);

@@ -4,8 +4,10 @@
 // CTA takes an equal share of all tiles: a batch of any lengths, or one long sequence, fills the GPU evenly without the host
 // knowing a length.  A share covers parts of one or several slices.  For each part a CTA forms a running softmax (maximum,
 // sum, un-normalised output) per query head; a slice that lies in one share is finished there, the parts of the others are
-// joined by join_kernel, in the order of the shares.  With scores, the logits go to scratch on the way and join_kernel, which
-// knows the normalisers, adds the weights to the rows' scores.
+// joined, in the order of the shares, by the CTA that is done with its part last (a counter per slice says so): one launch, where a
+// second kernel costs its launch and 3 to 4 us more on the GPU.  With scores there is one all the same: the logits go to scratch on
+// the way, and score_kernel, which knows the normalisers, adds the weights to the rows' scores.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include <algorithm>
@@ -15,11 +17,14 @@
 #include "d2o_paged.cuh"
 #include "d2o_tc.cuh"
 
+namespace cg = cooperative_groups;
+
 namespace d2o {
 
 constexpr int kPagedThreads = 256;
 constexpr int kPagedWarps = kPagedThreads / 32;
-constexpr int kPagedMinTiles = 4;            // least share of a CTA
+constexpr int kPagedClusters = 4;            // cluster sizes 1 (none), 2, 4, 8
+constexpr int kPagedMinTiles = 8;            // least share of a CTA: one tile per warp
 
 struct PagedDecodeArgs {
   PagedView p;
@@ -28,37 +33,52 @@ struct PagedDecodeArgs {
   const int32_t* positions;                  // [B], or NULL
   int window, n_sink;
   int ctas;                                  // CTAs of the first kernel
-  int4* desc;                                // per slice: first share, last share, which part of the first share; -1: finished there
-  float* lse2;                               // [slices][G] normalisers in the log2 domain of slices finished in one share
+  uint32_t* done;                            // per slice: parts that are written; zero between launches
+  float* lse2;                               // [slices][G] normalisers in the log2 domain (with scores)
   float* parts;                              // [ctas][2][G][D + 4]: output, maximum, sum, -; 0: the share's first part, 1: its last
   float* logits;                             // per row of the pools, G logits in the log2 domain (with scores)
 };
 
-// The shares.  `share` CTAs of `tot` tiles: share c holds the tiles [tot * c / share, tot * (c + 1) / share).
-__device__ __forceinline__ int shares_of(long long tot, int ctas) {
-  return (int)min((long long)ctas, (tot + kPagedMinTiles - 1) / kPagedMinTiles);
+// a / b; nearly always both fit 32 bits, and a division of 64 bits is a hundred instructions
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
-__device__ __forceinline__ long long share_begin(long long tot, int share, int c) { return tot * c / share; }
-__device__ __forceinline__ int share_of_tile(long long tot, int share, long long tile) {
-  int c = (int)(tile * share / tot);
-  while (share_begin(tot, share, c + 1) <= tile) ++c;
-  return c;
-}
+// The shares of all tiles: the first `more` CTAs take size + 1 of them, the others, up to `share`, size.
+struct PagedShares {
+  long long tot, size;
+  int share, more;
+  __device__ __forceinline__ PagedShares() {}
+  __device__ __forceinline__ PagedShares(long long tot_, int ctas) : tot(tot_) {
+    share = (int)min((long long)ctas, quotient(tot + kPagedMinTiles - 1, kPagedMinTiles));
+    size = share ? quotient(tot, share) : 0;
+    more = (int)(tot - size * share);
+  }
+  __device__ __forceinline__ long long begin(int c) const { return c * size + min(c, more); }
+  __device__ __forceinline__ int of_tile(long long tile) const {
+    const long long head = more * (size + 1);
+    return tile < head ? (int)quotient(tile, size + 1) : more + (int)quotient(tile - head, size);
+  }
+};
 
 // Where this CTA begins: tiles before its first slice, and that slice.  Every CTA adds up the tiles of all slices: a thread
 // those of consecutive slices, then a scan over the block.
 struct PagedStart {
-  long long tot;                             // tiles in all
+  PagedShares shares;
   long long before;                          // tiles ahead of `slice`
-  int slice, share;
+  int slice;                                 // -1: no share
 };
-__device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int c, long long* s_scan /* [threads + 1] */, int* s_found) {
+template <typename F>
+__device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int c, long long* s_scan /* [warps + 1] */, int* s_found, F&& short_table) {
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n_slices = p.B * p.Hkv, per = (n_slices + kPagedThreads - 1) / kPagedThreads;
   const int s0 = min(n_slices, tid * per), s1 = min(n_slices, s0 + per);
   long long mine = 0;
-  for (int s = s0; s < s1; ++s) mine += PagedSpan(p.len[s], p.reach(), a.window, a.n_sink).tiles;
+  for (int s = s0; s < s1; ++s) {
+    const int n = p.len[s];
+    mine += PagedSpan(n, p.reach(), a.window, a.n_sink).tiles;
+    if (c == 0 && n >= p.reach()) short_table(s);            // no row for the new token
+  }
   long long inc = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += t; }
@@ -68,8 +88,8 @@ __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int 
 #pragma unroll
   for (int w = 0; w < kPagedWarps; ++w) { if (w < warp) base += s_scan[w]; tot += s_scan[w]; }
   PagedStart r;
-  r.tot = tot; r.share = shares_of(tot, a.ctas); r.slice = -1; r.before = 0;
-  const long long first = c < r.share ? share_begin(tot, r.share, c) : tot;
+  r.shares = PagedShares(tot, a.ctas); r.slice = -1; r.before = 0;
+  const long long first = c < r.shares.share ? r.shares.begin(c) : tot;
   long long at = base + inc - mine;
   if (first >= at && first < at + mine) {                    // one thread
     int s = s0;
@@ -81,43 +101,193 @@ __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int 
     *s_found = s; s_scan[kPagedWarps] = at;
   }
   __syncthreads();
-  if (c < r.share) { r.slice = *s_found; r.before = s_scan[kPagedWarps]; }
+  if (c < r.shares.share) { r.slice = *s_found; r.before = s_scan[kPagedWarps]; }
   return r;
 }
 
-// The warps' results of one part (tiles i0 .. i1 of slice `sl`) become the slice's output, or a part for join_kernel.
-template <typename T, int D, int G, int LD>
-__device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, const PagedStart& start, int part, int sl, int i0, int i1, const PagedSpan& span,
-                                            long long before, const float* red, const float* s_m, const float* s_l, int ld) {
-  const PagedView& p = a.p;
-  const int c = blockIdx.x, b = sl / p.Hkv, h = sl % p.Hkv;
-  const bool whole = i0 == 0 && i1 == span.tiles;
-  float* to = a.parts + ((size_t)c * 2 + part) * G * (D + 4);
-  for (int i = threadIdx.x; i < G * D; i += kPagedThreads) {
-    const int g = i / D;
-    float mc = s_m[g];
-#pragma unroll
-    for (int w = 1; w < kPagedWarps; ++w) mc = fmaxf(mc, s_m[w * ld + g]);
-    float t = 0.f, lc = 0.f;
-#pragma unroll
-    for (int w = 0; w < kPagedWarps; ++w) {
-      const float m = s_m[w * ld + g], l = s_l[w * ld + g], f = m > -INFINITY ? exp2f(m - mc) : mc > -INFINITY ? 0.f : 1.f;
-      t = fmaf(red[(w * G + g) * LD + i % D], f, t);
-      lc = l != l ? NAN : fmaf(l, f, lc);
-    }
-    if (whole) {
-      ((T*)a.out)[((size_t)b * p.Hq + (size_t)h * G) * D + i] = Elem<T>::from_float(t / lc);
-      if (i % D == 0) a.lse2[sl * G + g] = mc + log2f(lc);
-    } else {
-      to[g * (D + 4) + i % D] = t;
-      if (i % D == 0) { to[g * (D + 4) + D] = mc; to[g * (D + 4) + D + 1] = lc; }
-    }
-  }
-  if (i0 == 0 && threadIdx.x == 0)
-    a.desc[sl] = whole ? make_int4(c, -1, 0, 0) : make_int4(c, share_of_tile(start.tot, start.share, before + span.tiles - 1), part, 0);
+// The share of a CTA in a cluster per slice: its first tile, and behind its last one, of the slice's.  -1: nothing to do.
+template <typename F>
+__device__ __forceinline__ PagedStart cluster_start(const PagedDecodeArgs& a, int& first, int& last, F&& short_table) {
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), r = (int)cluster.block_rank(), sl = (int)blockIdx.x / C, n = a.p.len[sl];
+  const PagedSpan span(n, a.p.reach(), a.window, a.n_sink);
+  first = span.tiles * r / C; last = span.tiles * (r + 1) / C;
+  if (n >= a.p.reach() && r == 0 && threadIdx.x == 0) short_table(sl);
+  PagedStart s;
+  s.slice = span.t < 0 ? -1 : sl; s.before = 0;
+  return s;
 }
 
+// A slice whose table has no row for the new token: NaN, by one thread.
 template <typename T, int D, int G>
+__device__ __forceinline__ void short_table_output(const PagedDecodeArgs& a, int sl) {
+  a.p.report(kPagedShortTable);
+  T* out = (T*)a.out + ((size_t)(sl / a.p.Hkv) * a.p.Hq + (size_t)(sl % a.p.Hkv) * G) * D;
+  for (int i = 0; i < G * D; ++i) out[i] = Elem<T>::from_float(NAN);
+}
+
+// Joins the parts c0 .. c1 of a slice (part `slot` of the first share, the first part of the others).  kPagedWarps / G warps per head,
+// each every so many parts, whose results are added in shared memory: the order is that of the shares whatever CTA does it.
+template <typename T, int D, int G>
+__device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int c0, int c1, int slot, float4* s_acc /* [warps][D / 4] */) {
+  constexpr int LPR = D / 4, RPW = 32 / LPR, W = kPagedWarps / G, STEP = W * RPW;        // lanes per row of D floats, rows of a warp, warps per head
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = warp / W, sub = warp % W, lig = lane % LPR;
+  auto part = [&](int c) { return a.parts + (((size_t)c * 2 + (c == c0 ? slot : 0)) * G + g) * (D + 4); };
+  // the largest maximum and the sum; the first 32 parts' maxima stay in registers
+  float m = -INFINITY, l = 0.f, m0 = -INFINITY;
+  for (int c = c0 + lane; c <= c1; c += 32) {
+    const float2 x = __ldcg(reinterpret_cast<const float2*>(part(c) + D));
+    const float mn = fmaxf(m, x.x);
+    l = (m > -INFINITY ? l * exp2f(m - mn) : l) + (x.x > -INFINITY ? x.y * exp2f(x.x - mn) : x.y);        // nothing finite: 0 or NaN
+    m = mn;
+    if (c < c0 + 32) m0 = x.x;
+  }
+  const float mc = warp_max(m);
+  l = warp_sum(m > -INFINITY ? l * exp2f(m - mc) : l);
+  float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int base = c0; base <= c1; base += 32) {
+    const float mx = base == c0 ? m0 : base + lane <= c1 ? __ldcg(part(base + lane) + D) : -INFINITY;
+    const float f = mx > -INFINITY ? exp2f(mx - mc) : 0.f;   // of part base + lane
+    const int n = min(32, c1 - base + 1);
+#pragma unroll 8
+    for (int i = 0; i < n; i += STEP) {
+      const int k = i + sub * RPW + lane / LPR;
+      const float w = __shfl_sync(0xffffffffu, f, k & 31);
+      if (k < n) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(part(base + k) + lig * 4));
+        t.x = fmaf(v.x, w, t.x); t.y = fmaf(v.y, w, t.y); t.z = fmaf(v.z, w, t.z); t.w = fmaf(v.w, w, t.w);
+      }
+    }
+  }
+  if (RPW == 2) {
+    t.x += __shfl_xor_sync(0xffffffffu, t.x, 16); t.y += __shfl_xor_sync(0xffffffffu, t.y, 16);
+    t.z += __shfl_xor_sync(0xffffffffu, t.z, 16); t.w += __shfl_xor_sync(0xffffffffu, t.w, 16);
+  }
+  if (lane < LPR) s_acc[warp * LPR + lane] = t;
+  if (a.logits && sub == 0 && lane == 0) a.lse2[sl * G + g] = mc + log2f(l);
+  __syncthreads();
+  if (sub == 0 && lane < LPR) {
+#pragma unroll
+    for (int i = 1; i < W; ++i) {
+      const float4 u = s_acc[(warp + i) * LPR + lane];
+      t.x += u.x; t.y += u.y; t.z += u.z; t.w += u.w;
+    }
+    T* out = (T*)a.out + ((size_t)(sl / a.p.Hkv) * a.p.Hq + (size_t)(sl % a.p.Hkv) * G + g) * D + lane * 4;
+    out[0] = Elem<T>::from_float(t.x / l); out[1] = Elem<T>::from_float(t.y / l);
+    out[2] = Elem<T>::from_float(t.z / l); out[3] = Elem<T>::from_float(t.w / l);
+  }
+}
+
+// Parts of slices that other shares continue: at most the share's first and its last.
+struct PagedOpen {
+  int n = 0, sl[2], c0[2], c1[2], slot[2];
+};
+
+// The warps' results of one part (tiles i0 .. i1 of slice `sl`) become the slice's output, or one of the parts to be joined.  s_m, s_l:
+// maxima and sums [warps][ld]; the maxima become the warps' factors.  CL: a part for join_cluster, in shared memory.  Begins and ends behind a barrier of the caller's.
+template <typename T, int D, int G, int LD, bool CL>
+__device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, const PagedStart& start, PagedOpen& open, float* swap, int part, int sl, int i0, int i1,
+                                            const PagedSpan& span, long long before, const float* red, float* s_m, float* s_l, int ld) {
+  const PagedView& p = a.p;
+  const int tid = threadIdx.x, c = blockIdx.x, b = sl / p.Hkv, h = sl % p.Hkv;
+  const bool whole = !CL && i0 == 0 && i1 == span.tiles;
+  float* to = CL ? swap : a.parts + ((size_t)c * 2 + part) * G * (D + 4);
+  if (tid < G) {
+    float m[kPagedWarps], mc = -INFINITY, lc = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPagedWarps; ++w) { m[w] = s_m[w * ld + tid]; mc = fmaxf(mc, m[w]); }
+#pragma unroll
+    for (int w = 0; w < kPagedWarps; ++w) {
+      const float l = s_l[w * ld + tid], f = m[w] > -INFINITY ? exp2f(m[w] - mc) : mc > -INFINITY ? 0.f : 1.f;
+      s_m[w * ld + tid] = f;
+      lc = l != l ? NAN : fmaf(l, f, lc);
+    }
+    s_l[tid] = lc;
+    if (!whole) *reinterpret_cast<float2*>(to + tid * (D + 4) + D) = make_float2(mc, lc);
+    else if (a.logits) a.lse2[sl * G + tid] = mc + log2f(lc);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < (G * D + kPagedThreads - 1) / kPagedThreads; ++x) {
+    const int i = x * kPagedThreads + tid, g = i / D;
+    if (G * D < kPagedThreads && i >= G * D) break;
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPagedWarps; ++w) t = fmaf(red[(w * G + g) * LD + i % D], s_m[w * ld + g], t);
+    if (whole) ((T*)a.out)[((size_t)b * p.Hq + (size_t)h * G) * D + i] = Elem<T>::from_float(t / s_l[g]);
+    else to[g * (D + 4) + i % D] = t;
+  }
+  if (!CL && !whole) {
+    // its parts: those of all shares that hold tiles of it; it is a share's second part unless it begins the share
+    const int x = open.n++;
+    open.sl[x] = sl;
+    open.c0[x] = start.shares.of_tile(before); open.c1[x] = start.shares.of_tile(before + span.tiles - 1);
+    open.slot[x] = before == start.shares.begin(open.c0[x]) ? 0 : 1;
+  }
+}
+
+// Joins the parts of a cluster's CTAs, which lie in their shared memory at `swap` ([G][D + 4]; `empty`: this CTA had no tiles).
+template <typename T, int D, int G>
+__device__ __forceinline__ void join_cluster(const PagedDecodeArgs& a, int sl, float* swap, bool empty) {
+  constexpr int MAX = 1 << (kPagedClusters - 1);
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = (int)cluster.num_blocks(), tid = threadIdx.x;
+  if (empty)
+    for (int i = tid; i < G * (D + 4); i += kPagedThreads) swap[i] = i % (D + 4) == D ? -INFINITY : 0.f;
+  cluster.sync();
+  if (cluster.block_rank() == 0) {
+#pragma unroll
+    for (int x = 0; x < (G * D + kPagedThreads - 1) / kPagedThreads; ++x) {
+      const int i = x * kPagedThreads + tid, g = i / D;
+      if (G * D < kPagedThreads && i >= G * D) break;
+      float2 ml[MAX];
+      float v[MAX], mc = -INFINITY, t = 0.f, l = 0.f;
+#pragma unroll
+      for (int r = 0; r < MAX; ++r) {
+        const float* y = cluster.map_shared_rank(swap, r < C ? r : 0) + g * (D + 4);
+        ml[r] = *reinterpret_cast<const float2*>(y + D);
+        v[r] = y[i % D];
+      }
+#pragma unroll
+      for (int r = 0; r < MAX; ++r)
+        if (r < C) mc = fmaxf(mc, ml[r].x);
+#pragma unroll
+      for (int r = 0; r < MAX; ++r) {
+        const float f = r < C ? (ml[r].x > -INFINITY ? exp2f(ml[r].x - mc) : mc > -INFINITY ? 0.f : 1.f) : 0.f;
+        t = r < C ? fmaf(v[r], f, t) : t;
+        l = r < C ? (ml[r].y != ml[r].y ? NAN : fmaf(ml[r].y, f, l)) : l;
+      }
+      ((T*)a.out)[((size_t)(sl / a.p.Hkv) * a.p.Hq + (size_t)(sl % a.p.Hkv) * G) * D + i] = Elem<T>::from_float(t / l);
+      if (a.logits && i % D == 0) a.lse2[sl * G + g] = mc + log2f(l);
+    }
+  }
+  cluster.sync();                                            // the others' parts have been read
+}
+
+// Counts the CTA's open parts, and joins the slices of which they were the last.
+template <typename T, int D, int G>
+__device__ __forceinline__ void close_parts(const PagedDecodeArgs& a, const PagedOpen& open, float* red, int* s_flag /* [2] */) {
+  if (open.n == 0) return;                                   // the caller's barrier lies behind the last part
+  if (threadIdx.x < open.n) {
+    const int x = threadIdx.x, sl = x ? open.sl[1] : open.sl[0], parts = x ? open.c1[1] - open.c0[1] : open.c1[0] - open.c0[0];
+    uint32_t before;
+    // the CTA's stores, ordered ahead of this thread by the barrier, become visible with the count; with the last count the others' are
+    asm volatile("fence.acq_rel.gpu;\n\tatom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.done + sl) : "memory");
+    const bool all = before == (uint32_t)parts;
+    if (all) a.done[sl] = 0u;                                // for the next launch
+    s_flag[x] = all;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int x = 0; x < open.n; ++x) {
+    if (!s_flag[x]) continue;
+    join_parts<T, D, G>(a, x ? open.sl[1] : open.sl[0], x ? open.c0[1] : open.c0[0], x ? open.c1[1] : open.c1[0], x ? open.slot[1] : open.slot[0],
+                        reinterpret_cast<float4*>(red));
+    __syncthreads();                                         // before the exchange area is written again
+  }
+}
+
+template <typename T, int D, int G, bool CL>
 __global__ void __launch_bounds__(kPagedThreads, 1)
 paged_decode_kernel(PagedDecodeArgs a) {
   start_dependents();
@@ -126,15 +296,19 @@ paged_decode_kernel(PagedDecodeArgs a) {
   extern __shared__ __align__(16) float red[];               // [warps][G][D]
   __shared__ float s_m[kPagedWarps][G], s_l[kPagedWarps][G];
   __shared__ long long s_scan[kPagedWarps + 1];
-  __shared__ int s_found;
+  __shared__ int s_found[2];
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int grp = lane / LPR, lig = lane % LPR, c = blockIdx.x;
-  const PagedStart start = paged_start(a, c, s_scan, &s_found);
+  auto short_table = [&](int sl) { short_table_output<T, D, G>(a, sl); };
+  int c_first = 0, c_last = 0;
+  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start(a, c, s_scan, s_found, short_table);
   if (start.slice < 0) return;
-  const long long first = share_begin(start.tot, start.share, c), last = share_begin(start.tot, start.share, c + 1);
+  const long long first = CL ? c_first : start.shares.begin(c), last = CL ? c_last : start.shares.begin(c + 1);
+  float* swap = red + kPagedWarps * G * D;                   // [G][D + 4], clusters
   long long before = start.before;
   int sl = start.slice;
+  PagedOpen open;
   for (long long at = first; at < last; ++sl) {
     const PagedSpan span(p.len[sl], p.reach(), a.window, a.n_sink);
     if (span.tiles == 0) continue;
@@ -259,11 +433,13 @@ paged_decode_kernel(PagedDecodeArgs a) {
       }
     }
     __syncthreads();
-    finish_part<T, D, G, D>(a, start, at == first ? 0 : 1, sl, i0, i1, span, before, red, &s_m[0][0], &s_l[0][0], G);
+    finish_part<T, D, G, D, CL>(a, start, open, swap, at == first ? 0 : 1, sl, i0, i1, span, before, red, &s_m[0][0], &s_l[0][0], G);
     __syncthreads();                                         // before the exchange area is written again
     at = before + i1;
     before += span.tiles;
   }
+  if (CL) join_cluster<T, D, G>(a, start.slice, swap, first == last);
+  else close_parts<T, D, G>(a, open, red, s_found);
 }
 
 // ------------------------------------------------------------------------------------ 16-bit caches: mma.sync
@@ -299,7 +475,7 @@ struct PagedCursor {
   __device__ __forceinline__ int row0() const { return span.row0((int)(at - before)); }
 };
 
-template <typename T, int D, int G>
+template <typename T, int D, int G, bool CL>
 __global__ void __launch_bounds__(kPagedThreads, 1)
 paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps) {
   start_dependents();
@@ -311,7 +487,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   __shared__ int s_row[kPagedWarps][kPagedStages];           // pool row of the stage's tile; -1: bad page
   __shared__ float s_m[kPagedWarps][8], s_l[kPagedWarps][8];
   __shared__ long long s_scan[kPagedWarps + 1];
-  __shared__ int s_found;
+  __shared__ int s_found[2];
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3, c = blockIdx.x;
   if (lane == 0)
@@ -319,10 +495,13 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   wait_for_prior_grid();
+  __syncwarp();
   asm volatile("fence.proxy.async.global;" ::: "memory");    // rows that kernels ahead wrote with ordinary stores are read by copies
-  const PagedStart start = paged_start(a, c, s_scan, &s_found);
+  auto short_table = [&](int sl) { short_table_output<T, D, G>(a, sl); };
+  int c_first = 0, c_last = 0;
+  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start(a, c, s_scan, s_found, short_table);
   if (start.slice < 0) return;
-  const long long first = share_begin(start.tot, start.share, c), last = share_begin(start.tot, start.share, c + 1);
+  const long long first = CL ? c_first : start.shares.begin(c), last = CL ? c_last : start.shares.begin(c + 1);
   unsigned char* my_ring = ring + (size_t)warp * kPagedStages * 2 * TILE;
 
   // ---- requests: the cursor is one tile ahead of them, its page number on the way
@@ -367,7 +546,12 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   PagedCursor cur(a, first, last, start.before, start.slice);            // at: first tile of the part
   long long mine = first + warp;                             // this warp's next tile
   int taken = 0;
+  PagedOpen open;
   bool lost = false;                                         // a wait ran out: NaN from here on
+  auto land = [&]() {                                        // sees the copies on their way land before the CTA may end
+    for (int i = max(0, asked - kPagedStages); i < asked; ++i)
+      if (!tc::mbar_wait(&s_full[warp][i % kPagedStages], (uint32_t)((i / kPagedStages) & 1))) break;
+  };
   while (cur.at < last) {
     const PagedSpan& span = cur.span;
     const int sl = cur.sl, b = sl / p.Hkv, h = sl % p.Hkv;
@@ -480,93 +664,33 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
       if (2 * tig < G) { to[0] = acc[i][0]; to[8] = acc[i][2]; }
       if (2 * tig + 1 < G) { to[LD] = acc[i][1]; to[LD + 8] = acc[i][3]; }
     }
+    if (CL && lost) land();                                  // the part goes to the ring's place
     __syncthreads();
-    finish_part<T, D, G, LD>(a, start, cur.at == first ? 0 : 1, sl, (int)(cur.at - cur.before), (int)(end - cur.before), span, cur.before, red, &s_m[0][0], &s_l[0][0], 8);
+    finish_part<T, D, G, LD, CL>(a, start, open, reinterpret_cast<float*>(paged_smem), cur.at == first ? 0 : 1, sl, (int)(cur.at - cur.before), (int)(end - cur.before), span, cur.before, red, &s_m[0][0], &s_l[0][0], 8);
     __syncthreads();                                         // before the exchange area is written again
     cur.at = end;
     cur.settle(a, last);
   }
-  if (lost)                                                  // see the copies on their way land before the CTA may end
-    for (int i = max(0, asked - kPagedStages); i < asked; ++i)
-      if (!tc::mbar_wait(&s_full[warp][i % kPagedStages], (uint32_t)((i / kPagedStages) & 1))) break;
+  if (CL) join_cluster<T, D, G>(a, start.slice, reinterpret_cast<float*>(paged_smem), first == last);
+  else close_parts<T, D, G>(a, open, red, s_found);
+  if (lost) land();
 }
 
-// Joins the parts of a slice (blockIdx.x): blockIdx.y < G one head of its output, a warp every eighth part; the others add the
-// weights to the scores of the slice's rows, divided over them.  (One CTA and one thread per element for all of a slice's parts, one
-// after another, took 21 us for 20 parts.)
-template <typename T, int D, int G>
+// Adds the weights to the scores of a slice's rows (blockIdx.x), divided over blockIdx.y.
+template <int G>
 __global__ void __launch_bounds__(kPagedThreads)
-join_kernel(PagedDecodeArgs a) {
+score_kernel(PagedDecodeArgs a) {
   start_dependents();
   wait_for_prior_grid();
-  constexpr int LPR = D / 4, GRPS = kPagedThreads / LPR, GPW = 32 / LPR;      // lanes per row of D floats, row groups, of a warp
-  __shared__ float s_lse[G];
-  __shared__ float4 s_acc[GRPS][LPR];
   const PagedView& p = a.p;
-  const int sl = blockIdx.x, b = sl / p.Hkv, h = sl % p.Hkv, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int n = p.len[sl];
-  if (n < 0) return;
-  const PagedSpan span(n, p.reach(), a.window, a.n_sink);
-  if (span.t < 0) {                                          // the table has no row for the new token
-    if (blockIdx.y == 0 && tid == 0) p.report(kPagedShortTable);
-    if (blockIdx.y < G && tid < D) ((T*)a.out)[((size_t)b * p.Hq + (size_t)h * G + blockIdx.y) * D + tid] = Elem<T>::from_float(NAN);
-    return;
-  }
-  const int4 desc = a.desc[sl];
-  const bool whole = desc.y < 0;
-  auto part = [&](int c, int g) { return a.parts + (((size_t)c * 2 + (c == desc.x ? desc.z : 0)) * G + g) * (D + 4); };
-  // largest maximum and sum of a head's parts, by a warp
-  auto total = [&](int g, float& m, float& l) {
-    m = -INFINITY; l = 0.f;
-    for (int c = desc.x + lane; c <= desc.y; c += 32) {
-      const float2 x = *reinterpret_cast<const float2*>(part(c, g) + D);
-      const float mn = fmaxf(m, x.x);
-      l = (m > -INFINITY ? l * exp2f(m - mn) : l) + (x.x > -INFINITY ? x.y * exp2f(x.x - mn) : x.y);      // nothing finite: 0 or NaN
-      m = mn;
-    }
-    const float mc = warp_max(m);
-    l = warp_sum(m > -INFINITY ? l * exp2f(m - mc) : l);
-    m = mc;
-  };
-  if (blockIdx.y < G) {
-    if (whole) return;
-    const int g = blockIdx.y, grp = tid / LPR, lig = tid % LPR;
-    float m, l;
-    total(g, m, l);                                          // by every warp: the same
-    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int c = desc.x + grp; c <= desc.y; c += GRPS) {
-      const float* x = part(c, g);
-      const float4 v = *reinterpret_cast<const float4*>(x + lig * 4);
-      const float f = x[D] > -INFINITY ? exp2f(x[D] - m) : 0.f;
-      t.x = fmaf(v.x, f, t.x); t.y = fmaf(v.y, f, t.y); t.z = fmaf(v.z, f, t.z); t.w = fmaf(v.w, f, t.w);
-    }
-    s_acc[grp][lig] = t;
-    __syncthreads();
-    if (tid < LPR) {
-      t = s_acc[0][tid];
-#pragma unroll
-      for (int i = 1; i < GRPS; ++i) { t.x += s_acc[i][tid].x; t.y += s_acc[i][tid].y; t.z += s_acc[i][tid].z; t.w += s_acc[i][tid].w; }
-      T* out = (T*)a.out + ((size_t)b * p.Hq + (size_t)h * G + g) * D + tid * 4;
-      out[0] = Elem<T>::from_float(t.x / l); out[1] = Elem<T>::from_float(t.y / l);
-      out[2] = Elem<T>::from_float(t.z / l); out[3] = Elem<T>::from_float(t.w / l);
-    }
-    return;
-  }
-  if (whole) {
-    if (tid < G) s_lse[tid] = a.lse2[sl * G + tid];
-  } else if (warp < G) {
-    float m, l;
-    total(warp, m, l);
-    if (lane == 0) s_lse[warp] = m + log2f(l);
-  }
-  __syncthreads();
+  const int sl = blockIdx.x, b = sl / p.Hkv, h = sl % p.Hkv;
+  const PagedSpan span(p.len[sl], p.reach(), a.window, a.n_sink);
+  if (span.t < 0) return;
   float lse[G];
 #pragma unroll
-  for (int g = 0; g < G; ++g) lse[g] = s_lse[g];
-  const int stride = (int)(gridDim.y - G) * kPagedThreads;
+  for (int g = 0; g < G; ++g) lse[g] = a.lse2[sl * G + g];
 #pragma unroll 2
-  for (int i = (int)(blockIdx.y - G) * kPagedThreads + tid; i < span.tiles * kPagedTile; i += stride) {
+  for (int i = (int)(blockIdx.y * kPagedThreads + threadIdx.x); i < span.tiles * kPagedTile; i += (int)gridDim.y * kPagedThreads) {
     const int r = span.row0(i / kPagedTile) + i % kPagedTile;
     if (!span.sees(r)) continue;
     const int page0 = p.page_row0(b, h, r);
@@ -587,15 +711,39 @@ join_kernel(PagedDecodeArgs a) {
 }
 
 // ------------------------------------------------------------------------------------ launch
+// CTAs per slice of a call whose slices get a cluster each, 1: shares of all tiles.  A cluster joins its parts through distributed shared
+// memory, in about a microsecond where counters and parts in global memory take five; but it knows no other slice, and one that is much
+// longer than the rest is left with its own CTAs.  So: calls whose slices get at least two CTAs each with one CTA per SM, up to eight
+// (the portable size), as long as what the table can hold gives a CTA at most 64 tiles (16-bit rows of d = 128: 512 KB, 10 us).
+static int paged_cluster(const PagedView& p, int n_slices, int sms) {
+  int C = 1;
+  while (2 * C <= 1 << (kPagedClusters - 1) && (long)n_slices * 2 * C <= sms) C *= 2;
+  return ((long long)p.max_pages << p.page_shift) <= 64ll * kPagedTile * C ? C : 1;
+}
+
+template <typename K, typename... A>
+static cudaError_t launch_shares(K kernel, const PagedDecodeArgs& a, int n_slices, int C, size_t smem, cudaStream_t st, const A&... args) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(C > 1 ? n_slices * C : a.ctas)); cfg.blockDim = dim3(kPagedThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = C > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a, args...);
+}
+
 template <typename T, int D, int G>
 static cudaError_t launch_one(const PagedDecodeArgs& a, cudaStream_t st) {
-  const int n_slices = a.p.B * a.p.Hkv;
+  const int n_slices = a.p.B * a.p.Hkv, C = paged_cluster(a.p, n_slices, a.ctas);
   cudaError_t e;
   if constexpr (sizeof(T) == 4) {
-    const size_t smem = (size_t)kPagedWarps * G * D * 4;
-    e = cudaFuncSetAttribute(paged_decode_kernel<T, D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    e = launch_behind(paged_decode_kernel<T, D, G>, dim3((unsigned)a.ctas), kPagedThreads, smem, st, a);
+    const size_t smem = (size_t)(kPagedWarps * G * D + G * (D + 4)) * 4;
+    e = C > 1 ? launch_shares(paged_decode_kernel<T, D, G, true>, a, n_slices, C, smem, st)
+              : launch_shares(paged_decode_kernel<T, D, G, false>, a, n_slices, C, smem, st);
   } else {
     const size_t smem = (size_t)kPagedWarps * (kPagedStages * 2 * kPagedTile * D * 2 + G * (D + 8) * 4);
     PagedMaps maps;
@@ -603,17 +751,15 @@ static cudaError_t launch_one(const PagedDecodeArgs& a, cudaStream_t st) {
     const uint64_t rows = (uint64_t)a.p.n_pages * a.p.Hkv << a.p.page_shift;
     if (!encode_rows_2d(&maps.k, dtype, a.p.k, rows, D, kPagedTile) || !encode_rows_2d(&maps.v, dtype, a.p.v, rows, D, kPagedTile))
       return cudaErrorNotSupported;
-    e = cudaFuncSetAttribute(paged_decode_tc_kernel<T, D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    e = launch_behind(paged_decode_tc_kernel<T, D, G>, dim3((unsigned)a.ctas), kPagedThreads, smem, st, a, maps);
+    e = C > 1 ? launch_shares(paged_decode_tc_kernel<T, D, G, true>, a, n_slices, C, smem, st, maps)
+              : launch_shares(paged_decode_tc_kernel<T, D, G, false>, a, n_slices, C, smem, st, maps);
   }
   if (e != cudaSuccess) return e;
-  int y = 0;                                                 // CTAs per slice that share the scores: up to four per SM, 1024 rows each at least
-  if (a.logits) {
-    const long long reach = (long long)a.p.max_pages << a.p.page_shift;
-    y = (int)std::max<long long>(1, std::min<long long>((4 * a.ctas + n_slices - 1) / n_slices, reach / 1024));
-  }
-  return launch_behind(join_kernel<T, D, G>, dim3((unsigned)n_slices, (unsigned)(G + y)), kPagedThreads, 0, st, a);
+  if (!a.logits) return cudaSuccess;
+  // CTAs per slice: up to four per SM, 1024 rows each at least
+  const long long reach = (long long)a.p.max_pages << a.p.page_shift;
+  const int y = (int)std::max<long long>(1, std::min<long long>((4 * a.ctas + n_slices - 1) / n_slices, reach / 1024));
+  return launch_behind(score_kernel<G>, dim3((unsigned)n_slices, (unsigned)y), kPagedThreads, 0, st, a);
 }
 
 template <typename T, int D>
@@ -637,7 +783,7 @@ cudaError_t launch_paged_decode(const PagedView& p, int dtype, int D, int window
   a.p = p;
   a.q = q; a.k = k; a.v = v; a.out = out; a.positions = positions; a.window = window; a.n_sink = n_sink;
   a.ctas = std::min(sms, kPagedCtas);
-  a.desc = reinterpret_cast<int4*>(scratch + s.desc);
+  a.done = reinterpret_cast<uint32_t*>(scratch + s.done);
   a.lse2 = reinterpret_cast<float*>(scratch + s.lse2);
   a.parts = reinterpret_cast<float*>(scratch + s.parts);
   a.logits = p.score ? reinterpret_cast<float*>(scratch + s.rows) : nullptr;
