@@ -100,9 +100,10 @@ cudaError_t launch_paged_append(const PagedView& p, int dtype, int D, int n_rows
 
 // ------------------------------------------------------------------------------------ evict
 constexpr int kEvictThreads = 512;
-constexpr int kEvictItems = 4;               // consecutive rows per thread in the ordered pass
+constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictKeys = 12288;            // rows of a CTA whose keys stay in shared memory
-constexpr int kEvictMaxCluster = 8;
+constexpr int kEvictMaxCluster = 16;
+constexpr int kEvictMoves = 4;               // moves of a group of lanes in flight
 
 struct EvictArgs {
   PagedView p;
@@ -124,13 +125,15 @@ struct EvictExchange {                       // read by the other CTAs of the cl
   int holes, movers, bad;
 };
 
-// One cluster per slice, its rows divided evenly over the CTAs.  (1) Keys.  (2) Radix select, 8 bits per round, of the lowest
-// key that stays: each CTA counts its rows, all add up the counts of all.  Where rows of that key stay only in part, rounds
-// over the positions of those follow (few slices have such ties, and then in a round or two a handful of rows).  (3) The rows below
-// the budget that go and the rows behind it that stay, each numbered in ascending order, form the moves; as many of one as of
-// the other, and sources and targets do not overlap, so that all moves run at once.  (4) The moves, divided over the
-// cluster.  What costs are the dependent steps: three or four cluster barriers for the select, two for the numbering.
-template <int ROWB>
+// One CTA or one cluster (CL) per slice, its rows divided evenly over the CTAs.  (1) Keys.  (2) Radix select, 8 bits per round, of the
+// lowest key that stays: each CTA counts its rows, all add up the counts of all.  The scores of a slice share their leading bits, so that
+// most lanes of a warp count in the same bin: they count together.  Where rows of the key stay only in part, rounds over
+// the positions of those follow.  (3) The rows below the budget that go and the rows behind it that stay, each numbered in ascending order
+// (every warp counts its own consecutive rows, one scan, every warp numbers them), form the moves; as many of one as of the other, and
+// sources and targets do not overlap, so that all moves run at once.  (4) The moves, divided over the cluster, several rows of a
+// group of lanes in flight.  What costs are the dependent steps.  us, counting lane by lane, numbering by block scans twice, one row in
+// flight, clusters of at most eight: 8 slices of 32768 rows to 6554 63, 256 slices of 2064 rows to 2048 31.
+template <int ROWB, bool CL>
 __global__ void __launch_bounds__(kEvictThreads)
 evict_kernel(EvictArgs a) {
   start_dependents();
@@ -138,12 +141,14 @@ evict_kernel(EvictArgs a) {
   constexpr int LPR = ROWB / 16, GRPS = kEvictThreads / LPR;
   extern __shared__ __align__(16) uint32_t s_keys[];
   __shared__ EvictExchange x;
-  __shared__ int s_warp[32], s_total, s_bin, s_need, s_count;
+  __shared__ int s_warp[kEvictWarps], s_holes[kEvictWarps], s_movers[kEvictWarps], s_bin, s_need, s_count;
   cg::cluster_group cluster = cg::this_cluster();
   const PagedView& p = a.p;
-  const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+  const int C = CL ? (int)cluster.num_blocks() : 1, rank = CL ? (int)cluster.block_rank() : 0;
   const int sl = blockIdx.x / C, b = sl / p.Hkv, h = sl % p.Hkv;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  auto sync_all = [&]() { if (CL) cluster.sync(); else __syncthreads(); };
+  auto of_rank = [&](int r) { return CL ? (const EvictExchange*)cluster.map_shared_rank(&x, r) : &x; };
   const int n = p.len[sl], budget = a.budgets[sl];
   // the same for all CTAs of the cluster
   if (n < 0) return;
@@ -162,6 +167,7 @@ evict_kernel(EvictArgs a) {
     return evict_key(p.score[at], p.pos[at], a.n_sink, first_recent);
   };
   auto key = [&](int i) { return i < kEvictKeys ? s_keys[i] : load_key(r0 + i); };
+#pragma unroll 4
   for (int i = tid; i < m; i += kEvictThreads) {
     const uint32_t k = load_key(r0 + i);
     if (i < kEvictKeys) s_keys[i] = k;
@@ -177,23 +183,37 @@ evict_kernel(EvictArgs a) {
     exact = false;
     for (int shift = 24; shift >= 0; shift -= 8, ++round) {
       int* hist = x.hist[round & 1];
-      for (int i = tid; i < m; i += kEvictThreads) {
-        uint32_t v;
-        if (value(i, v) && (v & mask) == prefix) atomicAdd(&hist[(v >> shift) & 255], 1);
+      for (int i = tid; i - lane < m; i += kEvictThreads) {  // whole warps
+        uint32_t v = 0;
+        const bool in = i < m && value(i, v) && (v & mask) == prefix;
+        const int bin = (v >> shift) & 255;
+        const unsigned who = __ballot_sync(0xffffffffu, in);
+        if (who == 0) continue;
+        const int lead = __ffs(who) - 1, first = __shfl_sync(0xffffffffu, bin, lead);
+        const unsigned same = __ballot_sync(0xffffffffu, in && bin == first);
+        if (lane == lead) atomicAdd(&hist[first], __popc(same));
+        if (in && bin != first) atomicAdd(&hist[bin], 1);
       }
-      cluster.sync();
+      sync_all();
       int c = 0;
-      if (tid < 256)
-        for (int r = 0; r < C; ++r) c += cluster.map_shared_rank(&x, r)->hist[round & 1][255 - tid];       // highest bin first
+      if (tid < 256) {
+        if (CL) {
+#pragma unroll 8
+          for (int r = 0; r < C; ++r) c += of_rank(r)->hist[round & 1][255 - tid];        // highest bin first
+        } else {
+          c = hist[255 - tid];
+        }
+      }
       // inclusive prefix over the 256 bins: eight warps
       int inc = c;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += t; }
       if (lane == 31 && warp < 8) s_warp[warp] = inc;
-      x.hist[(round + 1) & 1][tid & 255] = 0;                // read by all before the barrier above
+      if (tid >= 256) x.hist[(round + 1) & 1][tid - 256] = 0;            // read by all before the barrier above
       __syncthreads();
       if (tid < 256) {
-        for (int w = 0; w < warp; ++w) inc += s_warp[w];
+#pragma unroll
+        for (int w = 0; w < 7; ++w) inc += w < warp ? s_warp[w] : 0;
         if (inc >= need && inc - c < need) { s_bin = 255 - tid; s_need = need - (inc - c); s_count = c; }
       }
       __syncthreads();
@@ -206,10 +226,10 @@ evict_kernel(EvictArgs a) {
   bool exact;
   kth = select([&](int i, uint32_t& v) { v = key(i); return true; }, exact);
   bool bad = false;
-  for (int r = 0; r < C; ++r) bad |= cluster.map_shared_rank(&x, r)->bad != 0;
+  for (int r = 0; r < C; ++r) bad |= of_rank(r)->bad != 0;
   if (bad) {                                                 // the same for all
     if (tid == 0 && rank == 0) p.report(kPagedBadPage);
-    cluster.sync();                                          // our exchange area may still be read
+    sync_all();                                              // our exchange area may still be read
     return;
   }
   if (!exact) {
@@ -225,86 +245,95 @@ evict_kernel(EvictArgs a) {
     if (!by_pos || k != kth) return k >= kth;
     return ~(uint32_t)p.pos[pool_row(r0 + i)] >= inv_pos;
   };
-  // ---- number the rows below the budget that go (holes) and those behind it that stay (movers)
-  auto numbered = [&](auto&& hole, auto&& mover) {
-    int holes = 0, movers = 0;
-    for (int base = 0; base < m; base += kEvictItems * kEvictThreads) {
-      int is_hole = 0, is_mover = 0;
-#pragma unroll
-      for (int e = 0; e < kEvictItems; ++e) {
-        const int i = base + tid * kEvictItems + e;
-        if (i >= m) break;
-        const bool s = stays(i);
-        if (r0 + i < budget) { if (!s) is_hole |= 1 << e; }
-        else if (s) is_mover |= 1 << e;
-      }
-      // exclusive prefix over the block of both counts at once (each at most 2048)
-      const int mine = __popc(is_hole) | (__popc(is_mover) << 16);
-      int inc = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += t; }
-      __syncthreads();
-      if (lane == 31) s_warp[warp] = inc;
-      __syncthreads();
-      if (warp == 0) {
-        const int w = lane < kEvictThreads / 32 ? s_warp[lane] : 0;
-        int winc = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const int t = __shfl_up_sync(0xffffffffu, winc, o); if (lane >= o) winc += t; }
-        s_warp[lane] = winc - w;
-        if (lane == 31) s_total = winc;
-      }
-      __syncthreads();
-      const int before = inc - mine + s_warp[warp];
-      int nh = holes + (before & 0xffff), nm = movers + (before >> 16);
-#pragma unroll
-      for (int e = 0; e < kEvictItems; ++e) {
-        const int r = r0 + base + tid * kEvictItems + e;
-        if (is_hole >> e & 1) hole(nh++, r);
-        if (is_mover >> e & 1) mover(nm++, r);
-      }
-      holes += s_total & 0xffff; movers += s_total >> 16;
+  // ---- number the rows below the budget that go (holes) and those behind it that stay (movers): each warp its own consecutive rows
+  const int per = (m + kEvictWarps - 1) / kEvictWarps, w0 = min(m, warp * per), w1 = min(m, w0 + per);
+  auto each = [&](auto&& f) {                                // f(row, its hole, its mover bits among the warp's 32)
+    for (int base = w0; base < w1; base += 32) {
+      const int i = base + lane;
+      const bool in = i < w1, s = in && stays(i), low = r0 + i < budget;
+      f(r0 + i, __ballot_sync(0xffffffffu, in && low && !s), __ballot_sync(0xffffffffu, s && !low));
     }
-    if (tid == 0) { x.holes = holes; x.movers = movers; }
   };
-  numbered([](int, int) {}, [](int, int) {});
-  cluster.sync();
-  int h0 = 0, m0 = 0, nh = 0, nm = 0;
-  for (int r = 0; r < C; ++r) {
-    const EvictExchange* y = cluster.map_shared_rank(&x, r);
-    if (r < rank) { h0 += y->holes; m0 += y->movers; }
-    nh += y->holes; nm += y->movers;
+  int holes = 0, movers = 0;
+  each([&](int, unsigned hb, unsigned mb) { holes += __popc(hb); movers += __popc(mb); });
+  if (lane == 0) { s_holes[warp] = holes; s_movers[warp] = movers; }
+  __syncthreads();
+  int h0 = 0, m0 = 0, nh = 0, nm = 0;                        // before this warp's; all
+#pragma unroll
+  for (int w = 0; w < kEvictWarps; ++w) {
+    if (w < warp) { h0 += s_holes[w]; m0 += s_movers[w]; }
+    nh += s_holes[w]; nm += s_movers[w];
   }
-  cluster.sync();                                            // before the counts are written again
+  if (CL) {
+    if (tid == 0) { x.holes = nh; x.movers = nm; }
+    cluster.sync();
+    nh = nm = 0;
+    for (int r = 0; r < C; ++r) {
+      const EvictExchange* y = of_rank(r);
+      const int yh = y->holes, ym = y->movers;
+      if (r < rank) { h0 += yh; m0 += ym; }
+      nh += yh; nm += ym;
+    }
+  }
   const int moves = min(nh, nm);                             // equal, unless positions stand twice
-  numbered([&](int k, int r) { if (h0 + k < moves) a.moves[pool_row(h0 + k)].y = pool_row(r); },
-           [&](int k, int r) { if (m0 + k < moves) a.moves[pool_row(m0 + k)].x = pool_row(r); });
-  cluster.sync();
+  const unsigned below = (1u << lane) - 1u;
+  each([&](int r, unsigned hb, unsigned mb) {
+    const int hk = h0 + __popc(hb & below), mk = m0 + __popc(mb & below);
+    if ((hb >> lane & 1) && hk < moves) a.moves[pool_row(hk)].y = pool_row(r);
+    if ((mb >> lane & 1) && mk < moves) a.moves[pool_row(mk)].x = pool_row(r);
+    h0 += __popc(hb); m0 += __popc(mb);
+  });
+  sync_all();
   // ---- the moves
   const int grp = tid / LPR, lig = tid % LPR;
-  for (int k = rank * GRPS + grp; k < moves; k += C * GRPS) {
-    const int2 mv = a.moves[pool_row(k)];
-    const size_t from = (size_t)mv.x * ROWB + lig * 16, to = (size_t)mv.y * ROWB + lig * 16;
-    const uint4 kv = ld_stream_v4((const char*)p.k + from), vv = ld_stream_v4((const char*)p.v + from);
-    *reinterpret_cast<uint4*>((char*)p.k + to) = kv;
-    *reinterpret_cast<uint4*>((char*)p.v + to) = vv;
-    if (lig == 0) { p.pos[mv.y] = p.pos[mv.x]; p.score[mv.y] = p.score[mv.x]; }
+  for (int k0 = rank * GRPS + grp; k0 < moves; k0 += kEvictMoves * C * GRPS) {
+    int2 mv[kEvictMoves];
+    uint4 kv[kEvictMoves], vv[kEvictMoves];
+    int ps[kEvictMoves];
+    float sc[kEvictMoves];
+#pragma unroll
+    for (int u = 0; u < kEvictMoves; ++u) {
+      const int k = k0 + u * C * GRPS;
+      mv[u] = k < moves ? a.moves[pool_row(k)] : make_int2(-1, -1);
+    }
+#pragma unroll
+    for (int u = 0; u < kEvictMoves; ++u)
+      if (mv[u].x >= 0) {
+        const size_t from = (size_t)mv[u].x * ROWB + lig * 16;
+        kv[u] = ld_stream_v4((const char*)p.k + from);
+        vv[u] = ld_stream_v4((const char*)p.v + from);
+        if (lig == 0) { ps[u] = p.pos[mv[u].x]; sc[u] = p.score[mv[u].x]; }
+      }
+#pragma unroll
+    for (int u = 0; u < kEvictMoves; ++u)
+      if (mv[u].x >= 0) {
+        const size_t to = (size_t)mv[u].y * ROWB + lig * 16;
+        *reinterpret_cast<uint4*>((char*)p.k + to) = kv[u];
+        *reinterpret_cast<uint4*>((char*)p.v + to) = vv[u];
+        if (lig == 0) { p.pos[mv[u].y] = ps[u]; p.score[mv[u].y] = sc[u]; }
+      }
   }
 }
 
-template <int ROWB>
+template <int ROWB, bool CL>
 static cudaError_t launch_evict(const EvictArgs& a, int n_slices, int C, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(evict_kernel<ROWB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictKeys * 4);
+  cudaError_t e = cudaFuncSetAttribute(evict_kernel<ROWB, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictKeys * 4);
+  if (e == cudaSuccess && C > 8) e = cudaFuncSetAttribute(evict_kernel<ROWB, CL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(n_slices * C)); cfg.blockDim = dim3(kEvictThreads); cfg.dynamicSmemBytes = kEvictKeys * 4; cfg.stream = st;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = C; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr; cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, evict_kernel<ROWB>, a);
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = C; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = CL ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, evict_kernel<ROWB, CL>, a);
+}
+
+template <int ROWB>
+static cudaError_t launch_evict(const EvictArgs& a, int n_slices, int C, cudaStream_t st) {
+  return C > 1 ? launch_evict<ROWB, true>(a, n_slices, C, st) : launch_evict<ROWB, false>(a, n_slices, 1, st);
 }
 
 cudaError_t launch_paged_evict(const PagedView& p, int dtype, int D, const int32_t* budgets, const int32_t* next_pos, int n_sink,
@@ -315,8 +344,8 @@ cudaError_t launch_paged_evict(const PagedView& p, int dtype, int D, const int32
   const int n_slices = p.B * p.Hkv;
   const PagedScratch s(n_slices, p.Hq / p.Hkv, D, (size_t)p.n_pages * p.Hkv << p.page_shift, true);
   const EvictArgs a = {p, budgets, next_pos, reinterpret_cast<int2*>(scratch + s.rows), n_sink, window};
-  int C = 1;                                                 // one wave of clusters
-  while (2 * C <= kEvictMaxCluster && (long)n_slices * 2 * C <= 2l * sms) C *= 2;
+  int C = 1;                                                 // one CTA per SM
+  while (2 * C <= kEvictMaxCluster && (long)n_slices * 2 * C <= sms) C *= 2;
   const int rowb = D * (dtype == D2O_F32 ? 4 : 2);
   return rowb == 128 ? launch_evict<128>(a, n_slices, C, st) : rowb == 256 ? launch_evict<256>(a, n_slices, C, st)
                                                                            : launch_evict<512>(a, n_slices, C, st);
