@@ -104,6 +104,7 @@ constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictKeys = 12288;            // rows of a CTA whose keys stay in shared memory
 constexpr int kEvictMaxCluster = 16;
 constexpr int kEvictMoves = 4;               // moves of a group of lanes in flight
+constexpr int kEvictFew = kEvictThreads;     // rows in question that are ranked one by one instead of by further rounds
 
 struct EvictArgs {
   PagedView p;
@@ -122,19 +123,22 @@ __device__ __forceinline__ uint32_t evict_key(float score, int pos, int n_sink, 
 
 struct EvictExchange {                       // read by the other CTAs of the cluster
   int hist[2][256];
-  int holes, movers, bad;
+  int holes, movers, bad, few;
+  unsigned long long last;                   // the lowest (key, position) that stays, of the first CTA
+  unsigned long long list[kEvictFew];        // rows in question, of the first CTA
 };
 
 // One CTA or one cluster (CL) per slice, its rows divided evenly over the CTAs.  (1) Keys.  (2) Radix select, 8 bits per round, of the
 // lowest key that stays: each CTA counts its rows, all add up the counts of all.  The scores of a slice share their leading bits, so that
-// most lanes of a warp count in the same bin: they count together.  Where rows of the key stay only in part, rounds over
-// the positions of those follow.  (3) The rows below the budget that go and the rows behind it that stay, each numbered in ascending order
+// most lanes of a warp count in the same bin: they count together.  As soon as the border lies among a few hundred rows, those are
+// gathered with their positions and ranked one by one (nearly always behind the second round); where more than that are equal to the last
+// bit, rounds over their positions follow.  (3) The rows below the budget that go and the rows behind it that stay, each numbered in ascending order
 // (every warp counts its own consecutive rows, one scan, every warp numbers them), form the moves; as many of one as of the other, and
 // sources and targets do not overlap, so that all moves run at once.  (4) The moves, divided over the cluster, several rows of a
 // group of lanes in flight.  What costs are the dependent steps.  us, counting lane by lane, numbering by block scans twice, one row in
 // flight, clusters of at most eight: 8 slices of 32768 rows to 6554 63, 256 slices of 2064 rows to 2048 31.
 template <int ROWB, bool CL>
-__global__ void __launch_bounds__(kEvictThreads)
+__global__ void __launch_bounds__(kEvictThreads, 2)
 evict_kernel(EvictArgs a) {
   start_dependents();
   wait_for_prior_grid();
@@ -158,7 +162,7 @@ evict_kernel(EvictArgs a) {
   const long long first_recent = (long long)a.next_pos[b] - a.window;
   const int chunk = (n + C - 1) / C, r0 = min(n, rank * chunk), m = min(n, r0 + chunk) - r0;      // this CTA's rows r0 .. r0 + m
   if (tid < 256) { x.hist[0][tid] = 0; x.hist[1][tid] = 0; }
-  if (tid == 0) { x.holes = x.movers = x.bad = 0; }
+  if (tid == 0) { x.holes = x.movers = x.bad = x.few = 0; x.last = 0; }
   __syncthreads();
   auto pool_row = [&](int r) { const int row0 = p.page_row0(b, h, r); return row0 < 0 ? -1 : row0 + p.in_page(r); };
   auto load_key = [&](int r) {
@@ -167,38 +171,54 @@ evict_kernel(EvictArgs a) {
     return evict_key(p.score[at], p.pos[at], a.n_sink, first_recent);
   };
   auto key = [&](int i) { return i < kEvictKeys ? s_keys[i] : load_key(r0 + i); };
-#pragma unroll 4
-  for (int i = tid; i < m; i += kEvictThreads) {
-    const uint32_t k = load_key(r0 + i);
-    if (i < kEvictKeys) s_keys[i] = k;
+  for (int i0 = tid; i0 < m; i0 += 8 * kEvictThreads) {       // eight rows of a thread side by side: three dependent loads each
+    int at[8], ps[8];
+    float sc[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) at[u] = i0 + u * kEvictThreads < m ? pool_row(r0 + i0 + u * kEvictThreads) : -2;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (at[u] >= 0) { sc[u] = p.score[at[u]]; ps[u] = p.pos[at[u]]; }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int i = i0 + u * kEvictThreads;
+      if (at[u] == -1) x.bad = 1;
+      if (at[u] >= 0 && i < kEvictKeys) s_keys[i] = evict_key(sc[u], ps[u], a.n_sink, first_recent);
+    }
   }
   __syncthreads();
   // ---- the lowest (key, position) that stays, from the top eight bits down
   uint32_t kth = 0, inv_pos = 0;                             // rows above (kth, inv_pos), or equal, stay
-  int need = budget;
-  bool by_pos = false;
+  int need = budget, in_bin = n;                             // rows of the bin in question that stay, and in all
   int round = 0;
-  auto select = [&](auto&& value, bool& exact) {             // 32 bits; value(i, v): is row i still in question, and its bits
-    uint32_t prefix = 0, mask = 0;
-    exact = false;
-    for (int shift = 24; shift >= 0; shift -= 8, ++round) {
+  // 32 bits of the rows in question (value(i, v): is row i one, and its bits); true: the border is found
+  auto select = [&](auto&& value, uint32_t& prefix, uint32_t& mask) {
+    prefix = mask = 0;
+    for (int shift = 24; shift >= 0; shift -= 8) {
       int* hist = x.hist[round & 1];
-      for (int i = tid; i - lane < m; i += kEvictThreads) {  // whole warps
-        uint32_t v = 0;
-        const bool in = i < m && value(i, v) && (v & mask) == prefix;
-        const int bin = (v >> shift) & 255;
-        const unsigned who = __ballot_sync(0xffffffffu, in);
-        if (who == 0) continue;
-        const int lead = __ffs(who) - 1, first = __shfl_sync(0xffffffffu, bin, lead);
-        const unsigned same = __ballot_sync(0xffffffffu, in && bin == first);
-        if (lane == lead) atomicAdd(&hist[first], __popc(same));
-        if (in && bin != first) atomicAdd(&hist[bin], 1);
+      for (int i0 = tid; i0 - lane < m; i0 += 4 * kEvictThreads) {           // whole warps, four rows of a thread side by side
+        uint32_t v[4];
+        bool in[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int i = i0 + u * kEvictThreads;
+          v[u] = 0;
+          in[u] = i < m && value(i, v[u]) && (v[u] & mask) == prefix;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int bin = (v[u] >> shift) & 255;
+          const unsigned who = __ballot_sync(0xffffffffu, in[u]);
+          const int lead = who ? __ffs(who) - 1 : 0, first = __shfl_sync(0xffffffffu, bin, lead);
+          const unsigned same = __ballot_sync(0xffffffffu, in[u] && bin == first);
+          if (in[u] && (lane == lead || bin != first)) atomicAdd(&hist[bin], lane == lead ? __popc(same) : 1);
+        }
       }
       sync_all();
       int c = 0;
       if (tid < 256) {
         if (CL) {
-#pragma unroll 8
+#pragma unroll 16
           for (int r = 0; r < C; ++r) c += of_rank(r)->hist[round & 1][255 - tid];        // highest bin first
         } else {
           c = hist[255 - tid];
@@ -218,13 +238,15 @@ evict_kernel(EvictArgs a) {
       }
       __syncthreads();
       prefix |= (uint32_t)s_bin << shift; mask |= 255u << shift;
-      need = s_need;
-      if (need == s_count) { exact = true; ++round; break; }     // all rows of this bin stay: the lower bits do not matter
+      need = s_need; in_bin = s_count;
+      ++round;
+      if (need == in_bin) return true;                       // all rows of this bin stay: the lower bits do not matter
+      if (in_bin <= kEvictFew) return false;
     }
-    return prefix;
+    return false;
   };
-  bool exact;
-  kth = select([&](int i, uint32_t& v) { v = key(i); return true; }, exact);
+  uint32_t mask = 0;
+  bool exact = select([&](int i, uint32_t& v) { v = key(i); return true; }, kth, mask), by_pos = !exact;
   bool bad = false;
   for (int r = 0; r < C; ++r) bad |= of_rank(r)->bad != 0;
   if (bad) {                                                 // the same for all
@@ -232,18 +254,49 @@ evict_kernel(EvictArgs a) {
     sync_all();                                              // our exchange area may still be read
     return;
   }
-  if (!exact) {
-    by_pos = true;
-    inv_pos = select([&](int i, uint32_t& v) {
+  auto inverse_pos = [&](int i) { return ~(uint32_t)p.pos[pool_row(r0 + i)]; };
+  EvictExchange* const lead_x = CL ? cluster.map_shared_rank(&x, 0) : &x;
+  auto gather = [&](unsigned long long v) {                  // to the first CTA's list: in_bin rows
+    const int at = atomicAdd(&lead_x->few, 1);
+    if (at < kEvictFew) lead_x->list[at] = v;
+  };
+  if (!exact && in_bin > kEvictFew) {                        // equal to the last bit: by their positions
+    uint32_t pos_mask;
+    exact = select([&](int i, uint32_t& v) {
       if (key(i) != kth) return false;
-      v = ~(uint32_t)p.pos[pool_row(r0 + i)];
+      v = inverse_pos(i);
       return true;
-    }, exact);
+    }, inv_pos, pos_mask);
+    if (in_bin > kEvictFew) exact = true;                    // positions that stand many times over
+    if (!exact)
+      for (int i = tid; i < m; i += kEvictThreads)
+        if (key(i) == kth) {
+          const uint32_t v = inverse_pos(i);
+          if ((v & pos_mask) == inv_pos) gather((unsigned long long)kth << 32 | v);
+        }
+  } else if (!exact) {
+    for (int i = tid; i < m; i += kEvictThreads) {
+      const uint32_t k = key(i);
+      if ((k & mask) == kth) gather((unsigned long long)k << 32 | inverse_pos(i));
+    }
+  }
+  if (!exact) {                                              // the border among the rows of the list
+    sync_all();
+    if (rank == 0 && tid < in_bin) {
+      const unsigned long long mine = x.list[tid];
+      int above = 0, equal = 0;
+#pragma unroll 8
+      for (int i = 0; i < in_bin; ++i) { above += x.list[i] > mine; equal += x.list[i] == mine; }
+      if (above < need && need <= above + equal) x.last = mine;
+    }
+    sync_all();
+    const unsigned long long last = of_rank(0)->last;
+    kth = (uint32_t)(last >> 32); inv_pos = (uint32_t)last;
   }
   auto stays = [&](int i) {
     const uint32_t k = key(i);
     if (!by_pos || k != kth) return k >= kth;
-    return ~(uint32_t)p.pos[pool_row(r0 + i)] >= inv_pos;
+    return inverse_pos(i) >= inv_pos;
   };
   // ---- number the rows below the budget that go (holes) and those behind it that stay (movers): each warp its own consecutive rows
   const int per = (m + kEvictWarps - 1) / kEvictWarps, w0 = min(m, warp * per), w1 = min(m, w0 + per);
@@ -286,16 +339,22 @@ evict_kernel(EvictArgs a) {
   sync_all();
   // ---- the moves
   const int grp = tid / LPR, lig = tid % LPR;
+  int2 next[kEvictMoves];                                    // the following moves, read beside the rows of these
+  auto look = [&](int k0) {
+#pragma unroll
+    for (int u = 0; u < kEvictMoves; ++u) {
+      const int k = k0 + u * C * GRPS;
+      next[u] = k < moves ? a.moves[pool_row(k)] : make_int2(-1, -1);
+    }
+  };
+  look(rank * GRPS + grp);
   for (int k0 = rank * GRPS + grp; k0 < moves; k0 += kEvictMoves * C * GRPS) {
     int2 mv[kEvictMoves];
     uint4 kv[kEvictMoves], vv[kEvictMoves];
     int ps[kEvictMoves];
     float sc[kEvictMoves];
 #pragma unroll
-    for (int u = 0; u < kEvictMoves; ++u) {
-      const int k = k0 + u * C * GRPS;
-      mv[u] = k < moves ? a.moves[pool_row(k)] : make_int2(-1, -1);
-    }
+    for (int u = 0; u < kEvictMoves; ++u) mv[u] = next[u];
 #pragma unroll
     for (int u = 0; u < kEvictMoves; ++u)
       if (mv[u].x >= 0) {
@@ -304,6 +363,7 @@ evict_kernel(EvictArgs a) {
         vv[u] = ld_stream_v4((const char*)p.v + from);
         if (lig == 0) { ps[u] = p.pos[mv[u].x]; sc[u] = p.score[mv[u].x]; }
       }
+    look(k0 + kEvictMoves * C * GRPS);
 #pragma unroll
     for (int u = 0; u < kEvictMoves; ++u)
       if (mv[u].x >= 0) {
