@@ -66,6 +66,7 @@ struct PagedStart {
   PagedShares shares;
   long long before;                          // tiles ahead of `slice`
   int slice;                                 // -1: no share
+  int n;                                     // rows that it holds
 };
 template <typename F>
 __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int c, long long* s_scan /* [warps + 1] */, int* s_found, F&& short_table) {
@@ -88,7 +89,7 @@ __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int 
 #pragma unroll
   for (int w = 0; w < kPagedWarps; ++w) { if (w < warp) base += s_scan[w]; tot += s_scan[w]; }
   PagedStart r;
-  r.shares = PagedShares(tot, a.ctas); r.slice = -1; r.before = 0;
+  r.shares = PagedShares(tot, a.ctas); r.slice = -1; r.before = 0; r.n = 0;
   const long long first = c < r.shares.share ? r.shares.begin(c) : tot;
   long long at = base + inc - mine;
   if (first >= at && first < at + mine) {                    // one thread
@@ -98,10 +99,10 @@ __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int 
       if (first < at + tiles) break;
       at += tiles;
     }
-    *s_found = s; s_scan[kPagedWarps] = at;
+    s_found[0] = s; s_found[1] = p.len[s]; s_scan[kPagedWarps] = at;
   }
   __syncthreads();
-  if (c < r.shares.share) { r.slice = *s_found; r.before = s_scan[kPagedWarps]; }
+  if (c < r.shares.share) { r.slice = s_found[0]; r.n = s_found[1]; r.before = s_scan[kPagedWarps]; }
   return r;
 }
 
@@ -114,7 +115,7 @@ __device__ __forceinline__ PagedStart cluster_start(const PagedDecodeArgs& a, in
   first = span.tiles * r / C; last = span.tiles * (r + 1) / C;
   if (n >= a.p.reach() && r == 0 && threadIdx.x == 0) short_table(sl);
   PagedStart s;
-  s.slice = span.t < 0 ? -1 : sl; s.before = 0;
+  s.slice = span.t < 0 ? -1 : sl; s.before = 0; s.n = n;
   return s;
 }
 
@@ -133,6 +134,14 @@ __device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int
   constexpr int LPR = D / 4, RPW = 32 / LPR, W = kPagedWarps / G, STEP = W * RPW;        // lanes per row of D floats, rows of a warp, warps per head
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = warp / W, sub = warp % W, lig = lane % LPR;
   auto part = [&](int c) { return a.parts + (((size_t)c * 2 + (c == c0 ? slot : 0)) * G + g) * (D + 4); };
+  // the first outputs on their way beside the maxima
+  constexpr int AHEAD = 4;
+  float4 ahead[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int k = i * STEP + sub * RPW + lane / LPR;
+    ahead[i] = c0 + k <= c1 && k < 32 ? __ldcg(reinterpret_cast<const float4*>(part(c0 + k) + lig * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
   // the largest maximum and the sum; the first 32 parts' maxima stay in registers
   float m = -INFINITY, l = 0.f, m0 = -INFINITY;
   for (int c = c0 + lane; c <= c1; c += 32) {
@@ -149,8 +158,16 @@ __device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int
     const float mx = base == c0 ? m0 : base + lane <= c1 ? __ldcg(part(base + lane) + D) : -INFINITY;
     const float f = mx > -INFINITY ? exp2f(mx - mc) : 0.f;   // of part base + lane
     const int n = min(32, c1 - base + 1);
-#pragma unroll 8
-    for (int i = 0; i < n; i += STEP) {
+    if (base == c0) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int k = i * STEP + sub * RPW + lane / LPR;
+        const float w = __shfl_sync(0xffffffffu, f, k & 31);
+        if (k < n) { t.x = fmaf(ahead[i].x, w, t.x); t.y = fmaf(ahead[i].y, w, t.y); t.z = fmaf(ahead[i].z, w, t.z); t.w = fmaf(ahead[i].w, w, t.w); }
+      }
+    }
+#pragma unroll 4
+    for (int i = base == c0 ? AHEAD * STEP : 0; i < n; i += STEP) {
       const int k = i + sub * RPW + lane / LPR;
       const float w = __shfl_sync(0xffffffffu, f, k & 31);
       if (k < n) {
@@ -272,7 +289,7 @@ __device__ __forceinline__ void close_parts(const PagedDecodeArgs& a, const Page
     const int x = threadIdx.x, sl = x ? open.sl[1] : open.sl[0], parts = x ? open.c1[1] - open.c0[1] : open.c1[0] - open.c0[0];
     uint32_t before;
     // the CTA's stores, ordered ahead of this thread by the barrier, become visible with the count; with the last count the others' are
-    asm volatile("fence.acq_rel.gpu;\n\tatom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.done + sl) : "memory");
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.done + sl) : "memory");
     const bool all = before == (uint32_t)parts;
     if (all) a.done[sl] = 0u;                                // for the next launch
     s_flag[x] = all;
@@ -461,14 +478,17 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
 // A warp's place in the tiles of its CTA: tile `at` of all, in slice `sl`, which begins at tile `before`.
 struct PagedCursor {
   long long at, before;
-  int sl;
+  int sl, b, h;
   PagedSpan span;
-  __device__ __forceinline__ PagedCursor(const PagedDecodeArgs& a, long long at_, long long last, long long before_, int sl_)
-      : at(at_), before(before_), sl(sl_), span(a.p.len[sl_], a.p.reach(), a.window, a.n_sink) { settle(a, last); }
+  __device__ __forceinline__ PagedCursor(const PagedDecodeArgs& a, const PagedStart& start, long long at_, long long last)
+      : at(at_), before(start.before), sl(start.slice), b(start.slice / a.p.Hkv), h(start.slice % a.p.Hkv), span(start.n, a.p.reach(), a.window, a.n_sink) {
+    settle(a, last);
+  }
   __device__ __forceinline__ void settle(const PagedDecodeArgs& a, long long last) {
     while (at < last && at >= before + span.tiles) {
       before += span.tiles;
       ++sl;
+      if (++h == a.p.Hkv) { h = 0; ++b; }
       span = PagedSpan(a.p.len[sl], a.p.reach(), a.window, a.n_sink);
     }
   }
@@ -505,37 +525,48 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   unsigned char* my_ring = ring + (size_t)warp * kPagedStages * 2 * TILE;
 
   // ---- requests: the cursor is one tile ahead of them, its page number on the way
-  PagedCursor ask(a, first + warp, last, start.before, start.slice);
+  PagedCursor ask(a, start, first + warp, last);
   auto page_row = [&](const PagedCursor& x) {
     if (x.at >= last) return -1;
-    const int r = x.row0(), row0 = p.page_row0(x.sl / p.Hkv, x.sl % p.Hkv, r);
+    const int r = x.row0(), row0 = p.page_row0(x.b, x.h, r);
     return row0 < 0 ? -1 : row0 + p.in_page(r);
   };
-  int asked = 0, ask_row = page_row(ask);
-  auto request = [&]() {
-    if (ask.at >= last) return;
+  int asked = 0, ask_row = -1;
+  auto copy = [&](long long at, int row) {                   // of the tile at pool row `row`
+    if (at >= last) return;
     const int s = asked % kPagedStages;
     if (lane == 0) {
-      s_row[warp][s] = ask_row;
+      s_row[warp][s] = row;
       unsigned char* to = my_ring + s * 2 * TILE;
-      if (ask_row >= 0) {
+      if (row >= 0) {
         tc::mbar_expect_tx(&s_full[warp][s], 2 * TILE);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
-          tc::tma_load_2d(to + h * kPagedTile * 128, &maps.k, h * 64, ask_row, &s_full[warp][s]);
-          tc::tma_load_2d(to + TILE + h * kPagedTile * 128, &maps.v, h * 64, ask_row, &s_full[warp][s]);
+          tc::tma_load_2d(to + h * kPagedTile * 128, &maps.k, h * 64, row, &s_full[warp][s]);
+          tc::tma_load_2d(to + TILE + h * kPagedTile * 128, &maps.v, h * 64, row, &s_full[warp][s]);
         }
       } else {
         tc::mbar_arrive(&s_full[warp][s]);
       }
     }
     ++asked;
+  };
+  auto request = [&]() {
+    if (ask.at >= last) return;
+    copy(ask.at, ask_row);
     ask.at += kPagedWarps;
     ask.settle(a, last);
     ask_row = page_row(ask);
   };
-#pragma unroll 1
-  for (int s = 0; s < kPagedStages; ++s) request();
+  {
+    int rows[kPagedStages];                                  // the first page numbers, side by side
+    long long at[kPagedStages];
+#pragma unroll
+    for (int s = 0; s < kPagedStages; ++s) { rows[s] = page_row(ask); at[s] = ask.at; ask.at += kPagedWarps; ask.settle(a, last); }
+    ask_row = page_row(ask);
+#pragma unroll
+    for (int s = 0; s < kPagedStages; ++s) copy(at[s], rows[s]);
+  }
 
   // ---- the parts of the share
   const float scale = (D == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
@@ -543,7 +574,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   uint32_t v_off[4];
 #pragma unroll
   for (int mt = 0; mt < 4; ++mt) v_off[mt] = (uint32_t)(krow * 128 + (((mt * 2 + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
-  PagedCursor cur(a, first, last, start.before, start.slice);            // at: first tile of the part
+  PagedCursor cur(a, start, first, last);            // at: first tile of the part
   long long mine = first + warp;                             // this warp's next tile
   int taken = 0;
   PagedOpen open;
@@ -554,7 +585,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   };
   while (cur.at < last) {
     const PagedSpan& span = cur.span;
-    const int sl = cur.sl, b = sl / p.Hkv, h = sl % p.Hkv;
+    const int sl = cur.sl, b = cur.b, h = cur.h;
     const long long end = min(last, cur.before + span.tiles);
     const T* k_new = (const T*)a.k + (size_t)sl * D;
     const T* v_new = (const T*)a.v + (size_t)sl * D;
@@ -689,7 +720,7 @@ score_kernel(PagedDecodeArgs a) {
   float lse[G];
 #pragma unroll
   for (int g = 0; g < G; ++g) lse[g] = a.lse2[sl * G + g];
-#pragma unroll 2
+#pragma unroll 4
   for (int i = (int)(blockIdx.y * kPagedThreads + threadIdx.x); i < span.tiles * kPagedTile; i += (int)gridDim.y * kPagedThreads) {
     const int r = span.row0(i / kPagedTile) + i % kPagedTile;
     if (!span.sees(r)) continue;
@@ -756,9 +787,9 @@ static cudaError_t launch_one(const PagedDecodeArgs& a, cudaStream_t st) {
   }
   if (e != cudaSuccess) return e;
   if (!a.logits) return cudaSuccess;
-  // CTAs per slice: up to four per SM, 1024 rows each at least
+  // CTAs per slice: up to eight per SM, a row per thread at least
   const long long reach = (long long)a.p.max_pages << a.p.page_shift;
-  const int y = (int)std::max<long long>(1, std::min<long long>((4 * a.ctas + n_slices - 1) / n_slices, reach / 1024));
+  const int y = (int)std::max<long long>(1, std::min<long long>((8 * a.ctas + n_slices - 1) / n_slices, reach / kPagedThreads));
   return launch_behind(score_kernel<G>, dim3((unsigned)n_slices, (unsigned)y), kPagedThreads, 0, st, a);
 }
 
