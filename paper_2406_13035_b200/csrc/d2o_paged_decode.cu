@@ -135,7 +135,7 @@ __device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = warp / W, sub = warp % W, lig = lane % LPR;
   auto part = [&](int c) { return a.parts + (((size_t)c * 2 + (c == c0 ? slot : 0)) * G + g) * (D + 4); };
   // the first outputs on their way beside the maxima
-  constexpr int AHEAD = 4;
+  constexpr int AHEAD = 2;
   float4 ahead[AHEAD];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) {
@@ -166,7 +166,7 @@ __device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int
         if (k < n) { t.x = fmaf(ahead[i].x, w, t.x); t.y = fmaf(ahead[i].y, w, t.y); t.z = fmaf(ahead[i].z, w, t.z); t.w = fmaf(ahead[i].w, w, t.w); }
       }
     }
-#pragma unroll 4
+#pragma unroll 2
     for (int i = base == c0 ? AHEAD * STEP : 0; i < n; i += STEP) {
       const int k = i + sub * RPW + lane / LPR;
       const float w = __shfl_sync(0xffffffffu, f, k & 31);
@@ -197,7 +197,14 @@ __device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int
 
 // Parts of slices that other shares continue: at most the share's first and its last.
 struct PagedOpen {
-  int n = 0, sl[2], c0[2], c1[2], slot[2];
+  int n = 0, sl[2], tiles[2];
+  long long before[2];
+  __device__ __forceinline__ void add(int sl_, long long before_, int tiles_) {
+    // two constant places, not an indexed one: registers
+    if (n == 0) { sl[0] = sl_; before[0] = before_; tiles[0] = tiles_; }
+    else { sl[1] = sl_; before[1] = before_; tiles[1] = tiles_; }
+    ++n;
+  }
 };
 
 // The warps' results of one part (tiles i0 .. i1 of slice `sl`) become the slice's output, or one of the parts to be joined.  s_m, s_l:
@@ -234,13 +241,7 @@ __device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, const Page
     if (whole) ((T*)a.out)[((size_t)b * p.Hq + (size_t)h * G) * D + i] = Elem<T>::from_float(t / s_l[g]);
     else to[g * (D + 4) + i % D] = t;
   }
-  if (!CL && !whole) {
-    // its parts: those of all shares that hold tiles of it; it is a share's second part unless it begins the share
-    const int x = open.n++;
-    open.sl[x] = sl;
-    open.c0[x] = start.shares.of_tile(before); open.c1[x] = start.shares.of_tile(before + span.tiles - 1);
-    open.slot[x] = before == start.shares.begin(open.c0[x]) ? 0 : 1;
-  }
+  if (!CL && !whole) open.add(sl, before, span.tiles);
 }
 
 // Joins the parts of a cluster's CTAs, which lie in their shared memory at `swap` ([G][D + 4]; `empty`: this CTA had no tiles).
@@ -283,23 +284,27 @@ __device__ __forceinline__ void join_cluster(const PagedDecodeArgs& a, int sl, f
 
 // Counts the CTA's open parts, and joins the slices of which they were the last.
 template <typename T, int D, int G>
-__device__ __forceinline__ void close_parts(const PagedDecodeArgs& a, const PagedOpen& open, float* red, int* s_flag /* [2] */) {
+__device__ __forceinline__ void close_parts(const PagedDecodeArgs& a, const PagedStart& start, const PagedOpen& open, float* red, int4* s_join /* [2] */) {
   if (open.n == 0) return;                                   // the caller's barrier lies behind the last part
+  // A slice's parts are those of all shares that hold tiles of it; it is a share's second part unless it begins the share.  Thread x
+  // looks after part x.
   if (threadIdx.x < open.n) {
-    const int x = threadIdx.x, sl = x ? open.sl[1] : open.sl[0], parts = x ? open.c1[1] - open.c0[1] : open.c1[0] - open.c0[0];
+    const int x = threadIdx.x, sl = x ? open.sl[1] : open.sl[0], tiles = x ? open.tiles[1] : open.tiles[0];
+    const long long first = x ? open.before[1] : open.before[0];
+    const int c0 = start.shares.of_tile(first), c1 = start.shares.of_tile(first + tiles - 1);
     uint32_t before;
     // the CTA's stores, ordered ahead of this thread by the barrier, become visible with the count; with the last count the others' are
     asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.done + sl) : "memory");
-    const bool all = before == (uint32_t)parts;
+    const bool all = before == (uint32_t)(c1 - c0);
     if (all) a.done[sl] = 0u;                                // for the next launch
-    s_flag[x] = all;
+    s_join[x] = make_int4(all ? sl : -1, c0, c1, first == start.shares.begin(c0) ? 0 : 1);
   }
   __syncthreads();
-#pragma unroll 1
+#pragma unroll 1                                             // code that is run once comes from far: half of it
   for (int x = 0; x < open.n; ++x) {
-    if (!s_flag[x]) continue;
-    join_parts<T, D, G>(a, x ? open.sl[1] : open.sl[0], x ? open.c0[1] : open.c0[0], x ? open.c1[1] : open.c1[0], x ? open.slot[1] : open.slot[0],
-                        reinterpret_cast<float4*>(red));
+    const int4 j = s_join[x];
+    if (j.x < 0) continue;
+    join_parts<T, D, G>(a, j.x, j.y, j.z, j.w, reinterpret_cast<float4*>(red));
     __syncthreads();                                         // before the exchange area is written again
   }
 }
@@ -314,6 +319,7 @@ paged_decode_kernel(PagedDecodeArgs a) {
   __shared__ float s_m[kPagedWarps][G], s_l[kPagedWarps][G];
   __shared__ long long s_scan[kPagedWarps + 1];
   __shared__ int s_found[2];
+  __shared__ int4 s_join[2];
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int grp = lane / LPR, lig = lane % LPR, c = blockIdx.x;
@@ -456,7 +462,7 @@ paged_decode_kernel(PagedDecodeArgs a) {
     before += span.tiles;
   }
   if (CL) join_cluster<T, D, G>(a, start.slice, swap, first == last);
-  else close_parts<T, D, G>(a, open, red, s_found);
+  else close_parts<T, D, G>(a, start, open, red, s_join);
 }
 
 // ------------------------------------------------------------------------------------ 16-bit caches: mma.sync
@@ -495,6 +501,64 @@ struct PagedCursor {
   __device__ __forceinline__ int row0() const { return span.row0((int)(at - before)); }
 };
 
+// Buffers for the warps' results: two where shared memory has the room
+__host__ __device__ constexpr int paged_buffers(int G) { return G <= 4 ? 2 : 1; }
+
+// One warp adds the results of all warps for one part ([warps][G][LD] outputs, [warps][G, even] maxima and sums): the slice's output, or a part
+// for the joins in `to` ([G][D + 4]).
+template <typename T, int D, int G, int LD>
+__device__ __forceinline__ void combine_warps(const PagedDecodeArgs& a, int sl, int b, int h, bool whole, float* to, const float* red, const float* s_m, const float* s_l) {
+  static_assert(kPagedWarps == 8, "eight lanes per head");
+  constexpr int LPR = D / 4, HEADS = 32 / LPR;               // lanes per row of D floats, heads at a time
+  const int lane = threadIdx.x & 31, lig = lane % LPR;
+  // lane w + 8 g: factor of warp w for head g (and g + 4), and the sums
+  float f[2], lc[2], mc[2];
+#pragma unroll
+  for (int e = 0; e < (G > 4 ? 2 : 1); ++e) {
+    const int at = (lane & 7) * (G + G % 2) + lane / 8 + 4 * e;
+    const bool head = lane / 8 + 4 * e < G;
+    const float m = head ? s_m[at] : -INFINITY;
+    float l = head ? s_l[at] : 0.f;
+    mc[e] = m;
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) mc[e] = fmaxf(mc[e], __shfl_xor_sync(0xffffffffu, mc[e], o));
+    f[e] = m > -INFINITY ? exp2f(m - mc[e]) : mc[e] > -INFINITY ? 0.f : 1.f;
+    l = l != l ? NAN : l * f[e];                             // a NaN sum of a bad page stays
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    lc[e] = l;
+    if ((lane & 7) == 0 && head) {
+      const int g = lane / 8 + 4 * e;
+      if (!whole) *reinterpret_cast<float2*>(to + g * (D + 4) + D) = make_float2(mc[e], l);
+      else if (a.logits) a.lse2[sl * G + g] = mc[e] + log2f(l);
+    }
+  }
+#pragma unroll
+  for (int g0 = 0; g0 < G; g0 += HEADS) {
+    const int g = g0 + lane / LPR;                           // of this lane
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int from = (g & 3) * 8;
+#pragma unroll
+    for (int w = 0; w < kPagedWarps; ++w) {
+      const float x = __shfl_sync(0xffffffffu, g0 < 4 ? f[0] : f[1], (from + w) & 31);
+      if (g < G) {
+        const float4 v = *reinterpret_cast<const float4*>(red + (w * G + g) * LD + lig * 4);
+        t.x = fmaf(v.x, x, t.x); t.y = fmaf(v.y, x, t.y); t.z = fmaf(v.z, x, t.z); t.w = fmaf(v.w, x, t.w);
+      }
+    }
+    const float l = __shfl_sync(0xffffffffu, g0 < 4 ? lc[0] : lc[1], from);
+    if (g < G) {
+      if (whole) {
+        T* out = (T*)a.out + ((size_t)b * a.p.Hq + (size_t)h * G + g) * D + lig * 4;
+        out[0] = Elem<T>::from_float(t.x / l); out[1] = Elem<T>::from_float(t.y / l);
+        out[2] = Elem<T>::from_float(t.z / l); out[3] = Elem<T>::from_float(t.w / l);
+      } else {
+        *reinterpret_cast<float4*>(to + g * (D + 4) + lig * 4) = t;
+      }
+    }
+  }
+}
+
 template <typename T, int D, int G, bool CL>
 __global__ void __launch_bounds__(kPagedThreads, 1)
 paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps) {
@@ -502,16 +566,20 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   constexpr int HALVES = D / 64, TILE = kPagedTile * D * 2, LD = D + 8;
   extern __shared__ __align__(1024) unsigned char paged_smem[];
   unsigned char* ring = paged_smem;                          // [warps][stages][K, V][D / 64][16 rows][128 B]
-  float* red = reinterpret_cast<float*>(paged_smem + (size_t)kPagedWarps * kPagedStages * 2 * TILE);       // [warps][G][LD]
-  __shared__ unsigned long long s_full[kPagedWarps][kPagedStages];
+  constexpr int BUFS = paged_buffers(G);
+  float* red = reinterpret_cast<float*>(paged_smem + (size_t)kPagedWarps * kPagedStages * 2 * TILE);       // [BUFS][warps][G][LD]
+  __shared__ unsigned long long s_full[kPagedWarps][kPagedStages], s_written[BUFS], s_free[BUFS];
   __shared__ int s_row[kPagedWarps][kPagedStages];           // pool row of the stage's tile; -1: bad page
-  __shared__ float s_m[kPagedWarps][8], s_l[kPagedWarps][8];
+  __shared__ float s_m[BUFS][kPagedWarps][G + G % 2], s_l[BUFS][kPagedWarps][G + G % 2];
   __shared__ long long s_scan[kPagedWarps + 1];
   __shared__ int s_found[2];
+  __shared__ int4 s_join[2];
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3, c = blockIdx.x;
   if (lane == 0)
     for (int s = 0; s < kPagedStages; ++s) tc::mbar_init(&s_full[warp][s], 1);
+  if (tid == 0)
+    for (int i = 0; i < BUFS; ++i) { tc::mbar_init(&s_written[i], kPagedWarps); tc::mbar_init(&s_free[i], 1); }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   wait_for_prior_grid();
@@ -576,7 +644,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   for (int mt = 0; mt < 4; ++mt) v_off[mt] = (uint32_t)(krow * 128 + (((mt * 2 + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
   PagedCursor cur(a, start, first, last);            // at: first tile of the part
   long long mine = first + warp;                             // this warp's next tile
-  int taken = 0;
+  int taken = 0, parts = 0;
   PagedOpen open;
   bool lost = false;                                         // a wait ran out: NaN from here on
   auto land = [&]() {                                        // sees the copies on their way land before the CTA may end
@@ -602,7 +670,6 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
       const int s = taken % kPagedStages;
       if (!lost && !tc::mbar_wait(&s_full[warp][s], (uint32_t)((taken / kPagedStages) & 1))) {
         lost = true;
-        if (lane == 0 && p.status) report_error(p.status, D2O_ERR_TIMEOUT, 0x9A6E3000u);
       }
       lost = __any_sync(0xffffffffu, lost);
       ++taken;
@@ -685,25 +752,45 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
       __syncwarp();
       request();
     }
-    // ---- join the warps
+    // ---- the warp's result goes to a buffer; the warp whose turn it is waits for all of them, the others go on
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) { l[0] += __shfl_xor_sync(0xffffffffu, l[0], o); l[1] += __shfl_xor_sync(0xffffffffu, l[1], o); }
-    if (gid == 0) { s_m[warp][2 * tig] = m[0]; s_m[warp][2 * tig + 1] = m[1]; s_l[warp][2 * tig] = l[0]; s_l[warp][2 * tig + 1] = l[1]; }
+    const int buf = parts % BUFS;
+    const uint32_t phase = (uint32_t)((parts / BUFS) & 1);
+    if (parts >= BUFS && !lost && !tc::mbar_wait(&s_free[buf], phase ^ 1)) lost = true;
+    float* mine_red = red + (size_t)buf * kPagedWarps * G * LD + warp * G * LD;
+    if (gid == 0 && 2 * tig < G) {
+      s_m[buf][warp][2 * tig] = m[0]; s_m[buf][warp][2 * tig + 1] = m[1];
+      s_l[buf][warp][2 * tig] = l[0]; s_l[buf][warp][2 * tig + 1] = l[1];
+    }
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      float* to = red + (warp * G + 2 * tig) * LD + i * 16 + gid;
+      float* to = mine_red + 2 * tig * LD + i * 16 + gid;
       if (2 * tig < G) { to[0] = acc[i][0]; to[8] = acc[i][2]; }
       if (2 * tig + 1 < G) { to[LD] = acc[i][1]; to[LD + 8] = acc[i][3]; }
     }
-    if (CL && lost) land();                                  // the part goes to the ring's place
-    __syncthreads();
-    finish_part<T, D, G, LD, CL>(a, start, open, reinterpret_cast<float*>(paged_smem), cur.at == first ? 0 : 1, sl, (int)(cur.at - cur.before), (int)(end - cur.before), span, cur.before, red, &s_m[0][0], &s_l[0][0], 8);
-    __syncthreads();                                         // before the exchange area is written again
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(&s_written[buf]);
+    const int i0 = (int)(cur.at - cur.before), i1 = (int)(end - cur.before);
+    const bool whole = !CL && i0 == 0 && i1 == span.tiles;
+    if (warp == parts % kPagedWarps) {
+      if (!lost && !tc::mbar_wait(&s_written[buf], phase)) lost = true;
+      if (CL && lost) land();                                // the part goes to the ring's place
+      float* to = CL ? reinterpret_cast<float*>(paged_smem) : a.parts + ((size_t)c * 2 + (cur.at == first ? 0 : 1)) * G * (D + 4);
+      combine_warps<T, D, G, LD>(a, sl, b, h, whole, to, red + (size_t)buf * kPagedWarps * G * LD, &s_m[buf][0][0], &s_l[buf][0][0]);
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(&s_free[buf]);
+    }
+    if (!CL && !whole) open.add(sl, cur.before, span.tiles);
+    ++parts;
     cur.at = end;
     cur.settle(a, last);
   }
+  lost = __any_sync(0xffffffffu, lost);
+  if (lost && lane == 0 && p.status) report_error(p.status, D2O_ERR_TIMEOUT, 0x9A6E3000u);
+  __syncthreads();                                           // the last parts are combined
   if (CL) join_cluster<T, D, G>(a, start.slice, reinterpret_cast<float*>(paged_smem), first == last);
-  else close_parts<T, D, G>(a, open, red, s_found);
+  else close_parts<T, D, G>(a, start, open, red, s_join);
   if (lost) land();
 }
 
@@ -776,7 +863,7 @@ static cudaError_t launch_one(const PagedDecodeArgs& a, cudaStream_t st) {
     e = C > 1 ? launch_shares(paged_decode_kernel<T, D, G, true>, a, n_slices, C, smem, st)
               : launch_shares(paged_decode_kernel<T, D, G, false>, a, n_slices, C, smem, st);
   } else {
-    const size_t smem = (size_t)kPagedWarps * (kPagedStages * 2 * kPagedTile * D * 2 + G * (D + 8) * 4);
+    const size_t smem = (size_t)kPagedWarps * (kPagedStages * 2 * kPagedTile * D * 2 + paged_buffers(G) * G * (D + 8) * 4);
     PagedMaps maps;
     const int dtype = cuda::std::is_same<T, __half>::value ? D2O_F16 : D2O_BF16;
     const uint64_t rows = (uint64_t)a.p.n_pages * a.p.Hkv << a.p.page_shift;
