@@ -360,8 +360,8 @@ d2o_status d2o_paged_append(const d2o_paged_cache* cache, int32_t n_rows, const 
  * that d2o_paged_evict has been through is no longer in the order of positions, so that a window has no meaning there.
  * q, out DEVICE [B, Hq, d]; k, v DEVICE [B, Hkv, d].  With pos and score: row t gets positions[b] (DEVICE int32 [B]; NULL: t),
  * its weight, summed over the query heads, as score, and every other row that is seen has its weight added to its score (Eq. 6
- * case 2).  A sequence whose table does not reach row t, or has a bad page number among the rows seen, gets NaN outputs in the
- * heads concerned and sets the error word.  Rows outside the view may hold anything.  The caller adds one to len.
+ * case 2).  A sequence whose table does not reach row t gets NaN outputs, and one that
+ * has a bad page number among the rows seen NaN outputs and scores, in the heads concerned; both set the error word.  Rows outside the view may hold anything.  The caller adds one to len.
  * The rows of all sequences together are divided evenly over the GPU, whatever the single lengths, and what was divided is
  * joined again in a fixed order: results do not change from run to run.  Asynchronous. */
 d2o_status d2o_paged_decode_step(const d2o_paged_cache* cache, int32_t window, int32_t n_sink, const void* q, const void* k,

@@ -409,6 +409,12 @@ def _arg(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> Optional
                       f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
+def _view(window: int, n_sink: int):
+    """ctypes would wrap a number of 32 bits and more."""
+    _need(0 <= window < 1 << 31 and 0 <= n_sink < 1 << 31, "window, n_sink: 0 .. 2^31 - 1")
+    return window, n_sink
+
+
 def _call(device: torch.device, what: str, fn, *args):
     """fn(*args, stream) with the tensors' device current: their stream is that device's current one."""
     if device.index == torch.cuda.current_device():
@@ -428,7 +434,7 @@ def d2o_prompt_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out:
     _need(Q.dim() == 4 and K.dim() == 4 and Q.dtype in DTYPE_CODE and Q.is_cuda, "Q, K: [B, H, P, d] on the GPU")
     b, hq, n, d = Q.shape
     hkv, dev = K.shape[1], Q.device
-    _call(dev, "d2o_prompt_attention", load_library().d2o_prompt_attention, DTYPE_CODE[Q.dtype], d, b, hq, hkv, n, window, n_sink,
+    _call(dev, "d2o_prompt_attention", load_library().d2o_prompt_attention, DTYPE_CODE[Q.dtype], d, b, hq, hkv, n, *_view(window, n_sink),
           _arg(Q, "Q", (b, hq, n, d), Q.dtype, dev), _arg(K, "K", (b, hkv, n, d), Q.dtype, dev),
           _arg(V, "V", (b, hkv, n, d), Q.dtype, dev), _arg(lens, "lens", (b,), torch.int32, dev),
           _arg(out, "out", (b, hq, n, d), Q.dtype, dev), _arg(lse, "lse", (b, hq, n), torch.float32, dev),
@@ -481,12 +487,13 @@ class D2OPagedCache:
                               positions: Optional[torch.Tensor] = None, window: int = 0, n_sink: int = 0):
         b, hq, hkv, d = self.shape
         dev, dt = self.device, self.dtype
-        _call(dev, "d2o_paged_decode_step", self.lib.d2o_paged_decode_step, self._ref, window, n_sink,
+        _call(dev, "d2o_paged_decode_step", self.lib.d2o_paged_decode_step, self._ref, *_view(window, n_sink),
               _arg(q, "q", (b, hq, d), dt, dev), _arg(k, "k", (b, hkv, d), dt, dev), _arg(v, "v", (b, hkv, d), dt, dev),
               _arg(positions, "positions", (b,), torch.int32, dev), _arg(out, "out", (b, hq, d), dt, dev), *self._scratch)
 
     def d2o_paged_evict(self, budgets: torch.Tensor, next_pos: torch.Tensor, *, n_sink: int = 0, window: int = 0):
         b, _, hkv, _ = self.shape
+        window, n_sink = _view(window, n_sink)
         _call(self.device, "d2o_paged_evict", self.lib.d2o_paged_evict, self._ref,
               _arg(budgets, "budgets", (b, hkv), torch.int32, self.device), _arg(next_pos, "next_pos", (b,), torch.int32, self.device),
               n_sink, window, *self._scratch)

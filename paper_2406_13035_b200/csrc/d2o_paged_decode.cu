@@ -21,8 +21,12 @@ namespace cg = cooperative_groups;
 
 namespace d2o {
 
-constexpr int kPagedThreads = 256;
-constexpr int kPagedWarps = kPagedThreads / 32;
+constexpr int kPagedThreads = 256;           // of score_kernel
+constexpr int kPagedWarpsF32 = 8;            // of a CTA
+// 16-bit caches: a warp's time per tile is latency (two instructions of ten issued), so that as many warps as shared memory has
+// rings of two tiles for, beside their results; eight heads leave room for eight warps, with three.
+__host__ __device__ constexpr int paged_warps(int G) { return G <= 4 ? 12 : 8; }
+__host__ __device__ constexpr int paged_stages(int G) { return G <= 4 ? 2 : 3; }
 constexpr int kPagedClusters = 4;            // cluster sizes 1 (none), 2, 4, 8
 constexpr int kPagedMinTiles = 8;            // least share of a CTA: one tile per warp
 
@@ -68,11 +72,11 @@ struct PagedStart {
   int slice;                                 // -1: no share
   int n;                                     // rows that it holds
 };
-template <typename F>
+template <int NW, typename F>
 __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int c, long long* s_scan /* [warps + 1] */, int* s_found, F&& short_table) {
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int n_slices = p.B * p.Hkv, per = (n_slices + kPagedThreads - 1) / kPagedThreads;
+  const int n_slices = p.B * p.Hkv, per = (n_slices + (NW * 32) - 1) / (NW * 32);
   const int s0 = min(n_slices, tid * per), s1 = min(n_slices, s0 + per);
   long long mine = 0;
   for (int s = s0; s < s1; ++s) {
@@ -87,7 +91,7 @@ __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int 
   __syncthreads();
   long long base = 0, tot = 0;
 #pragma unroll
-  for (int w = 0; w < kPagedWarps; ++w) { if (w < warp) base += s_scan[w]; tot += s_scan[w]; }
+  for (int w = 0; w < NW; ++w) { if (w < warp) base += s_scan[w]; tot += s_scan[w]; }
   PagedStart r;
   r.shares = PagedShares(tot, a.ctas); r.slice = -1; r.before = 0; r.n = 0;
   const long long first = c < r.shares.share ? r.shares.begin(c) : tot;
@@ -99,10 +103,10 @@ __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int 
       if (first < at + tiles) break;
       at += tiles;
     }
-    s_found[0] = s; s_found[1] = p.len[s]; s_scan[kPagedWarps] = at;
+    s_found[0] = s; s_found[1] = p.len[s]; s_scan[NW] = at;
   }
   __syncthreads();
-  if (c < r.shares.share) { r.slice = s_found[0]; r.n = s_found[1]; r.before = s_scan[kPagedWarps]; }
+  if (c < r.shares.share) { r.slice = s_found[0]; r.n = s_found[1]; r.before = s_scan[NW]; }
   return r;
 }
 
@@ -127,12 +131,13 @@ __device__ __forceinline__ void short_table_output(const PagedDecodeArgs& a, int
   for (int i = 0; i < G * D; ++i) out[i] = Elem<T>::from_float(NAN);
 }
 
-// Joins the parts c0 .. c1 of a slice (part `slot` of the first share, the first part of the others).  kPagedWarps / G warps per head,
+// Joins the parts c0 .. c1 of a slice (part `slot` of the first share, the first part of the others).  NW / G warps per head,
 // each every so many parts, whose results are added in shared memory: the order is that of the shares whatever CTA does it.
-template <typename T, int D, int G>
+template <typename T, int D, int G, int NW>
 __device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int c0, int c1, int slot, float4* s_acc /* [warps][D / 4] */) {
-  constexpr int LPR = D / 4, RPW = 32 / LPR, W = kPagedWarps / G, STEP = W * RPW;        // lanes per row of D floats, rows of a warp, warps per head
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = warp / W, sub = warp % W, lig = lane % LPR;
+  constexpr int LPR = D / 4, RPW = 32 / LPR, W = NW / G, STEP = W * RPW;        // lanes per row of D floats, rows of a warp, warps per head
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = min(warp / W, G - 1), sub = warp % W, lig = lane % LPR;
+  const bool spare = warp >= W * G;                          // more warps than heads take
   auto part = [&](int c) { return a.parts + (((size_t)c * 2 + (c == c0 ? slot : 0)) * G + g) * (D + 4); };
   // the first outputs on their way beside the maxima
   constexpr int AHEAD = 2;
@@ -181,9 +186,9 @@ __device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int
     t.z += __shfl_xor_sync(0xffffffffu, t.z, 16); t.w += __shfl_xor_sync(0xffffffffu, t.w, 16);
   }
   if (lane < LPR) s_acc[warp * LPR + lane] = t;
-  if (a.logits && sub == 0 && lane == 0) a.lse2[sl * G + g] = mc + log2f(l);
+  if (a.logits && sub == 0 && lane == 0 && !spare) a.lse2[sl * G + g] = mc + log2f(l);
   __syncthreads();
-  if (sub == 0 && lane < LPR) {
+  if (sub == 0 && lane < LPR && !spare) {
 #pragma unroll
     for (int i = 1; i < W; ++i) {
       const float4 u = s_acc[(warp + i) * LPR + lane];
@@ -217,11 +222,11 @@ __device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, const Page
   const bool whole = !CL && i0 == 0 && i1 == span.tiles;
   float* to = CL ? swap : a.parts + ((size_t)c * 2 + part) * G * (D + 4);
   if (tid < G) {
-    float m[kPagedWarps], mc = -INFINITY, lc = 0.f;
+    float m[kPagedWarpsF32], mc = -INFINITY, lc = 0.f;
 #pragma unroll
-    for (int w = 0; w < kPagedWarps; ++w) { m[w] = s_m[w * ld + tid]; mc = fmaxf(mc, m[w]); }
+    for (int w = 0; w < kPagedWarpsF32; ++w) { m[w] = s_m[w * ld + tid]; mc = fmaxf(mc, m[w]); }
 #pragma unroll
-    for (int w = 0; w < kPagedWarps; ++w) {
+    for (int w = 0; w < kPagedWarpsF32; ++w) {
       const float l = s_l[w * ld + tid], f = m[w] > -INFINITY ? exp2f(m[w] - mc) : mc > -INFINITY ? 0.f : 1.f;
       s_m[w * ld + tid] = f;
       lc = l != l ? NAN : fmaf(l, f, lc);
@@ -232,12 +237,12 @@ __device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, const Page
   }
   __syncthreads();
 #pragma unroll
-  for (int x = 0; x < (G * D + kPagedThreads - 1) / kPagedThreads; ++x) {
-    const int i = x * kPagedThreads + tid, g = i / D;
-    if (G * D < kPagedThreads && i >= G * D) break;
+  for (int x = 0; x < (G * D + (kPagedWarpsF32 * 32) - 1) / (kPagedWarpsF32 * 32); ++x) {
+    const int i = x * (kPagedWarpsF32 * 32) + tid, g = i / D;
+    if (G * D < (kPagedWarpsF32 * 32) && i >= G * D) break;
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < kPagedWarps; ++w) t = fmaf(red[(w * G + g) * LD + i % D], s_m[w * ld + g], t);
+    for (int w = 0; w < kPagedWarpsF32; ++w) t = fmaf(red[(w * G + g) * LD + i % D], s_m[w * ld + g], t);
     if (whole) ((T*)a.out)[((size_t)b * p.Hq + (size_t)h * G) * D + i] = Elem<T>::from_float(t / s_l[g]);
     else to[g * (D + 4) + i % D] = t;
   }
@@ -245,19 +250,19 @@ __device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, const Page
 }
 
 // Joins the parts of a cluster's CTAs, which lie in their shared memory at `swap` ([G][D + 4]; `empty`: this CTA had no tiles).
-template <typename T, int D, int G>
+template <typename T, int D, int G, int NW>
 __device__ __forceinline__ void join_cluster(const PagedDecodeArgs& a, int sl, float* swap, bool empty) {
   constexpr int MAX = 1 << (kPagedClusters - 1);
   cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), tid = threadIdx.x;
   if (empty)
-    for (int i = tid; i < G * (D + 4); i += kPagedThreads) swap[i] = i % (D + 4) == D ? -INFINITY : 0.f;
+    for (int i = tid; i < G * (D + 4); i += (NW * 32)) swap[i] = i % (D + 4) == D ? -INFINITY : 0.f;
   cluster.sync();
   if (cluster.block_rank() == 0) {
 #pragma unroll
-    for (int x = 0; x < (G * D + kPagedThreads - 1) / kPagedThreads; ++x) {
-      const int i = x * kPagedThreads + tid, g = i / D;
-      if (G * D < kPagedThreads && i >= G * D) break;
+    for (int x = 0; x < (G * D + (NW * 32) - 1) / (NW * 32); ++x) {
+      const int i = x * (NW * 32) + tid, g = i / D;
+      if (i >= G * D) break;
       float2 ml[MAX];
       float v[MAX], mc = -INFINITY, t = 0.f, l = 0.f;
 #pragma unroll
@@ -283,7 +288,7 @@ __device__ __forceinline__ void join_cluster(const PagedDecodeArgs& a, int sl, f
 }
 
 // Counts the CTA's open parts, and joins the slices of which they were the last.
-template <typename T, int D, int G>
+template <typename T, int D, int G, int NW>
 __device__ __forceinline__ void close_parts(const PagedDecodeArgs& a, const PagedStart& start, const PagedOpen& open, float* red, int4* s_join /* [2] */) {
   if (open.n == 0) return;                                   // the caller's barrier lies behind the last part
   // A slice's parts are those of all shares that hold tiles of it; it is a share's second part unless it begins the share.  Thread x
@@ -304,20 +309,20 @@ __device__ __forceinline__ void close_parts(const PagedDecodeArgs& a, const Page
   for (int x = 0; x < open.n; ++x) {
     const int4 j = s_join[x];
     if (j.x < 0) continue;
-    join_parts<T, D, G>(a, j.x, j.y, j.z, j.w, reinterpret_cast<float4*>(red));
+    join_parts<T, D, G, NW>(a, j.x, j.y, j.z, j.w, reinterpret_cast<float4*>(red));
     __syncthreads();                                         // before the exchange area is written again
   }
 }
 
 template <typename T, int D, int G, bool CL>
-__global__ void __launch_bounds__(kPagedThreads, 1)
+__global__ void __launch_bounds__(kPagedWarpsF32 * 32, 1)
 paged_decode_kernel(PagedDecodeArgs a) {
   start_dependents();
   wait_for_prior_grid();
   constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR, U = kPagedTile / RPW, QL = LPR / 4;
   extern __shared__ __align__(16) float red[];               // [warps][G][D]
-  __shared__ float s_m[kPagedWarps][G], s_l[kPagedWarps][G];
-  __shared__ long long s_scan[kPagedWarps + 1];
+  __shared__ float s_m[kPagedWarpsF32][G], s_l[kPagedWarpsF32][G];
+  __shared__ long long s_scan[kPagedWarpsF32 + 1];
   __shared__ int s_found[2];
   __shared__ int4 s_join[2];
   const PagedView& p = a.p;
@@ -325,10 +330,10 @@ paged_decode_kernel(PagedDecodeArgs a) {
   const int grp = lane / LPR, lig = lane % LPR, c = blockIdx.x;
   auto short_table = [&](int sl) { short_table_output<T, D, G>(a, sl); };
   int c_first = 0, c_last = 0;
-  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start(a, c, s_scan, s_found, short_table);
+  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start<kPagedWarpsF32>(a, c, s_scan, s_found, short_table);
   if (start.slice < 0) return;
   const long long first = CL ? c_first : start.shares.begin(c), last = CL ? c_last : start.shares.begin(c + 1);
-  float* swap = red + kPagedWarps * G * D;                   // [G][D + 4], clusters
+  float* swap = red + kPagedWarpsF32 * G * D;                   // [G][D + 4], clusters
   long long before = start.before;
   int sl = start.slice;
   PagedOpen open;
@@ -349,7 +354,7 @@ paged_decode_kernel(PagedDecodeArgs a) {
 #pragma unroll
       for (int e = 0; e < EPV; ++e) { qf[g][e] *= (D == 64 ? 0.125f : 0.08838834764831845f) * kLog2e; acc[g][e] = 0.f; }
     }
-    for (int i = i0 + warp; i < i1; i += kPagedWarps) {
+    for (int i = i0 + warp; i < i1; i += kPagedWarpsF32) {
       const int row0 = span.row0(i);
       const int page0 = p.page_row0(b, h, row0);
       const size_t prow = (size_t)(page0 < 0 ? 0 : page0) + p.in_page(row0);
@@ -461,18 +466,16 @@ paged_decode_kernel(PagedDecodeArgs a) {
     at = before + i1;
     before += span.tiles;
   }
-  if (CL) join_cluster<T, D, G>(a, start.slice, swap, first == last);
-  else close_parts<T, D, G>(a, start, open, red, s_join);
+  if (CL) join_cluster<T, D, G, kPagedWarpsF32>(a, start.slice, swap, first == last);
+  else close_parts<T, D, G, kPagedWarpsF32>(a, start, open, red, s_join);
 }
 
 // ------------------------------------------------------------------------------------ 16-bit caches: mma.sync
-// Every warp takes every eighth tile of its CTA's share, through a ring of its own in shared memory that tiled tensor maps fill (128-
-// byte swizzle; one lane asks for the tile three ahead, across slices): nothing waits for another warp but the end of a part.  Logits:
+// Every warp takes every twelfth (eighth) tile of its CTA's share, through a ring of its own in shared memory that tiled tensor maps fill (128-
+// byte swizzle; one lane asks for the tiles ahead, across slices): nothing waits for another warp but the end of a part.  Logits:
 // rows x heads = K q^T on m16n8k16 (the up to eight heads are the columns); outputs: d x heads = V^T P with the weights as two 16-bit
 // terms, so that they keep 16 (bf16) or 22 (fp16) bits.  Tiles at the edge of what is seen have their unseen value rows zeroed in shared
 // memory (0 * NaN), and the new token's row put in its place.
-constexpr int kPagedStages = 3;
-
 struct PagedMaps { CUtensorMap k, v; };
 
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
@@ -502,51 +505,50 @@ struct PagedCursor {
 };
 
 // Buffers for the warps' results: two where shared memory has the room
-__host__ __device__ constexpr int paged_buffers(int G) { return G <= 4 ? 2 : 1; }
+__host__ __device__ constexpr int paged_buffers(int G) { return G <= 2 ? 2 : 1; }
 
 // One warp adds the results of all warps for one part ([warps][G][LD] outputs, [warps][G, even] maxima and sums): the slice's output, or a part
 // for the joins in `to` ([G][D + 4]).
 template <typename T, int D, int G, int LD>
 __device__ __forceinline__ void combine_warps(const PagedDecodeArgs& a, int sl, int b, int h, bool whole, float* to, const float* red, const float* s_m, const float* s_l) {
-  static_assert(kPagedWarps == 8, "eight lanes per head");
-  constexpr int LPR = D / 4, HEADS = 32 / LPR;               // lanes per row of D floats, heads at a time
+  constexpr int WARPS = paged_warps(G);
+  static_assert(WARPS <= 16, "sixteen lanes per head");
+  constexpr int LPR = D / 4, HEADS = 32 / LPR, N = (G + 1) / 2;          // lanes per row of D floats, heads at a time; factors per lane
   const int lane = threadIdx.x & 31, lig = lane % LPR;
-  // lane w + 8 g: factor of warp w for head g (and g + 4), and the sums
-  float f[2], lc[2], mc[2];
+  // lane w + 16 (g % 2), entry g / 2: factor of warp w for head g, and the sum
+  float f[N], lc[N];
 #pragma unroll
-  for (int e = 0; e < (G > 4 ? 2 : 1); ++e) {
-    const int at = (lane & 7) * (G + G % 2) + lane / 8 + 4 * e;
-    const bool head = lane / 8 + 4 * e < G;
-    const float m = head ? s_m[at] : -INFINITY;
-    float l = head ? s_l[at] : 0.f;
-    mc[e] = m;
+  for (int e = 0; e < N; ++e) {
+    const int w = lane & 15, g = 2 * e + lane / 16;
+    const bool in = w < WARPS && g < G;
+    const float m = in ? s_m[w * (G + G % 2) + g] : -INFINITY;
+    float l = in ? s_l[w * (G + G % 2) + g] : 0.f, mc = m;
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) mc[e] = fmaxf(mc[e], __shfl_xor_sync(0xffffffffu, mc[e], o));
-    f[e] = m > -INFINITY ? exp2f(m - mc[e]) : mc[e] > -INFINITY ? 0.f : 1.f;
+    for (int o = 1; o < 16; o <<= 1) mc = fmaxf(mc, __shfl_xor_sync(0xffffffffu, mc, o));
+    f[e] = m > -INFINITY ? exp2f(m - mc) : mc > -INFINITY ? 0.f : 1.f;
     l = l != l ? NAN : l * f[e];                             // a NaN sum of a bad page stays
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    for (int o = 1; o < 16; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     lc[e] = l;
-    if ((lane & 7) == 0 && head) {
-      const int g = lane / 8 + 4 * e;
-      if (!whole) *reinterpret_cast<float2*>(to + g * (D + 4) + D) = make_float2(mc[e], l);
-      else if (a.logits) a.lse2[sl * G + g] = mc[e] + log2f(l);
+    if (w == 0 && g < G) {
+      if (!whole) *reinterpret_cast<float2*>(to + g * (D + 4) + D) = make_float2(mc, l);
+      else if (a.logits) a.lse2[sl * G + g] = mc + log2f(l);
     }
   }
 #pragma unroll
   for (int g0 = 0; g0 < G; g0 += HEADS) {
     const int g = g0 + lane / LPR;                           // of this lane
     float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int from = (g & 3) * 8;
+    const int from = (g & 1) * 16;
 #pragma unroll
-    for (int w = 0; w < kPagedWarps; ++w) {
-      const float x = __shfl_sync(0xffffffffu, g0 < 4 ? f[0] : f[1], (from + w) & 31);
+    for (int w = 0; w < WARPS; ++w) {
+      const float x = __shfl_sync(0xffffffffu, f[g0 / 2], from + w);
       if (g < G) {
         const float4 v = *reinterpret_cast<const float4*>(red + (w * G + g) * LD + lig * 4);
         t.x = fmaf(v.x, x, t.x); t.y = fmaf(v.y, x, t.y); t.z = fmaf(v.z, x, t.z); t.w = fmaf(v.w, x, t.w);
       }
     }
-    const float l = __shfl_sync(0xffffffffu, g0 < 4 ? lc[0] : lc[1], from);
+    const float l = __shfl_sync(0xffffffffu, lc[g0 / 2], from);
     if (g < G) {
       if (whole) {
         T* out = (T*)a.out + ((size_t)b * a.p.Hq + (size_t)h * G + g) * D + lig * 4;
@@ -560,26 +562,26 @@ __device__ __forceinline__ void combine_warps(const PagedDecodeArgs& a, int sl, 
 }
 
 template <typename T, int D, int G, bool CL>
-__global__ void __launch_bounds__(kPagedThreads, 1)
+__global__ void __launch_bounds__(paged_warps(G) * 32, 1)
 paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps) {
   start_dependents();
-  constexpr int HALVES = D / 64, TILE = kPagedTile * D * 2, LD = D + 8;
+  constexpr int WARPS = paged_warps(G), STAGES = paged_stages(G), HALVES = D / 64, TILE = kPagedTile * D * 2, LD = D + 8;
   extern __shared__ __align__(1024) unsigned char paged_smem[];
   unsigned char* ring = paged_smem;                          // [warps][stages][K, V][D / 64][16 rows][128 B]
   constexpr int BUFS = paged_buffers(G);
-  float* red = reinterpret_cast<float*>(paged_smem + (size_t)kPagedWarps * kPagedStages * 2 * TILE);       // [BUFS][warps][G][LD]
-  __shared__ unsigned long long s_full[kPagedWarps][kPagedStages], s_written[BUFS], s_free[BUFS];
-  __shared__ int s_row[kPagedWarps][kPagedStages];           // pool row of the stage's tile; -1: bad page
-  __shared__ float s_m[BUFS][kPagedWarps][G + G % 2], s_l[BUFS][kPagedWarps][G + G % 2];
-  __shared__ long long s_scan[kPagedWarps + 1];
+  float* red = reinterpret_cast<float*>(paged_smem + (size_t)WARPS * STAGES * 2 * TILE);       // [BUFS][warps][G][LD]
+  __shared__ unsigned long long s_full[WARPS][STAGES], s_written[BUFS], s_free[BUFS];
+  __shared__ int s_row[WARPS][STAGES];           // pool row of the stage's tile; -1: bad page
+  __shared__ float s_m[BUFS][WARPS][G + G % 2], s_l[BUFS][WARPS][G + G % 2];
+  __shared__ long long s_scan[WARPS + 1];
   __shared__ int s_found[2];
   __shared__ int4 s_join[2];
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3, c = blockIdx.x;
   if (lane == 0)
-    for (int s = 0; s < kPagedStages; ++s) tc::mbar_init(&s_full[warp][s], 1);
+    for (int s = 0; s < STAGES; ++s) tc::mbar_init(&s_full[warp][s], 1);
   if (tid == 0)
-    for (int i = 0; i < BUFS; ++i) { tc::mbar_init(&s_written[i], kPagedWarps); tc::mbar_init(&s_free[i], 1); }
+    for (int i = 0; i < BUFS; ++i) { tc::mbar_init(&s_written[i], WARPS); tc::mbar_init(&s_free[i], 1); }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   wait_for_prior_grid();
@@ -587,10 +589,10 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   asm volatile("fence.proxy.async.global;" ::: "memory");    // rows that kernels ahead wrote with ordinary stores are read by copies
   auto short_table = [&](int sl) { short_table_output<T, D, G>(a, sl); };
   int c_first = 0, c_last = 0;
-  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start(a, c, s_scan, s_found, short_table);
+  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start<WARPS>(a, c, s_scan, s_found, short_table);
   if (start.slice < 0) return;
   const long long first = CL ? c_first : start.shares.begin(c), last = CL ? c_last : start.shares.begin(c + 1);
-  unsigned char* my_ring = ring + (size_t)warp * kPagedStages * 2 * TILE;
+  unsigned char* my_ring = ring + (size_t)warp * STAGES * 2 * TILE;
 
   // ---- requests: the cursor is one tile ahead of them, its page number on the way
   PagedCursor ask(a, start, first + warp, last);
@@ -602,7 +604,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   int asked = 0, ask_row = -1;
   auto copy = [&](long long at, int row) {                   // of the tile at pool row `row`
     if (at >= last) return;
-    const int s = asked % kPagedStages;
+    const int s = asked % STAGES;
     if (lane == 0) {
       s_row[warp][s] = row;
       unsigned char* to = my_ring + s * 2 * TILE;
@@ -622,18 +624,18 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   auto request = [&]() {
     if (ask.at >= last) return;
     copy(ask.at, ask_row);
-    ask.at += kPagedWarps;
+    ask.at += WARPS;
     ask.settle(a, last);
     ask_row = page_row(ask);
   };
   {
-    int rows[kPagedStages];                                  // the first page numbers, side by side
-    long long at[kPagedStages];
+    int rows[STAGES];                                  // the first page numbers, side by side
+    long long at[STAGES];
 #pragma unroll
-    for (int s = 0; s < kPagedStages; ++s) { rows[s] = page_row(ask); at[s] = ask.at; ask.at += kPagedWarps; ask.settle(a, last); }
+    for (int s = 0; s < STAGES; ++s) { rows[s] = page_row(ask); at[s] = ask.at; ask.at += WARPS; ask.settle(a, last); }
     ask_row = page_row(ask);
 #pragma unroll
-    for (int s = 0; s < kPagedStages; ++s) copy(at[s], rows[s]);
+    for (int s = 0; s < STAGES; ++s) copy(at[s], rows[s]);
   }
 
   // ---- the parts of the share
@@ -648,8 +650,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   PagedOpen open;
   bool lost = false;                                         // a wait ran out: NaN from here on
   auto land = [&]() {                                        // sees the copies on their way land before the CTA may end
-    for (int i = max(0, asked - kPagedStages); i < asked; ++i)
-      if (!tc::mbar_wait(&s_full[warp][i % kPagedStages], (uint32_t)((i / kPagedStages) & 1))) break;
+    for (int i = max(0, asked - STAGES); i < asked; ++i)
+      if (!tc::mbar_wait(&s_full[warp][i % STAGES], (uint32_t)((i / STAGES) & 1))) break;
   };
   while (cur.at < last) {
     const PagedSpan& span = cur.span;
@@ -666,9 +668,9 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, acc[D / 16][4];      // of heads 2 tig, 2 tig + 1
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-    for (; mine < end; mine += kPagedWarps) {
-      const int s = taken % kPagedStages;
-      if (!lost && !tc::mbar_wait(&s_full[warp][s], (uint32_t)((taken / kPagedStages) & 1))) {
+    for (; mine < end; mine += WARPS) {
+      const int s = taken % STAGES;
+      if (!lost && !tc::mbar_wait(&s_full[warp][s], (uint32_t)((taken / STAGES) & 1))) {
         lost = true;
       }
       lost = __any_sync(0xffffffffu, lost);
@@ -758,7 +760,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     const int buf = parts % BUFS;
     const uint32_t phase = (uint32_t)((parts / BUFS) & 1);
     if (parts >= BUFS && !lost && !tc::mbar_wait(&s_free[buf], phase ^ 1)) lost = true;
-    float* mine_red = red + (size_t)buf * kPagedWarps * G * LD + warp * G * LD;
+    float* mine_red = red + (size_t)buf * WARPS * G * LD + warp * G * LD;
     if (gid == 0 && 2 * tig < G) {
       s_m[buf][warp][2 * tig] = m[0]; s_m[buf][warp][2 * tig + 1] = m[1];
       s_l[buf][warp][2 * tig] = l[0]; s_l[buf][warp][2 * tig + 1] = l[1];
@@ -773,11 +775,11 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     if (lane == 0) tc::mbar_arrive(&s_written[buf]);
     const int i0 = (int)(cur.at - cur.before), i1 = (int)(end - cur.before);
     const bool whole = !CL && i0 == 0 && i1 == span.tiles;
-    if (warp == parts % kPagedWarps) {
+    if (warp == parts % WARPS) {
       if (!lost && !tc::mbar_wait(&s_written[buf], phase)) lost = true;
       if (CL && lost) land();                                // the part goes to the ring's place
       float* to = CL ? reinterpret_cast<float*>(paged_smem) : a.parts + ((size_t)c * 2 + (cur.at == first ? 0 : 1)) * G * (D + 4);
-      combine_warps<T, D, G, LD>(a, sl, b, h, whole, to, red + (size_t)buf * kPagedWarps * G * LD, &s_m[buf][0][0], &s_l[buf][0][0]);
+      combine_warps<T, D, G, LD>(a, sl, b, h, whole, to, red + (size_t)buf * WARPS * G * LD, &s_m[buf][0][0], &s_l[buf][0][0]);
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&s_free[buf]);
     }
@@ -789,8 +791,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   lost = __any_sync(0xffffffffu, lost);
   if (lost && lane == 0 && p.status) report_error(p.status, D2O_ERR_TIMEOUT, 0x9A6E3000u);
   __syncthreads();                                           // the last parts are combined
-  if (CL) join_cluster<T, D, G>(a, start.slice, reinterpret_cast<float*>(paged_smem), first == last);
-  else close_parts<T, D, G>(a, start, open, red, s_join);
+  if (CL) join_cluster<T, D, G, WARPS>(a, start.slice, reinterpret_cast<float*>(paged_smem), first == last);
+  else close_parts<T, D, G, WARPS>(a, start, open, red, s_join);
   if (lost) land();
 }
 
@@ -840,11 +842,11 @@ static int paged_cluster(const PagedView& p, int n_slices, int sms) {
 }
 
 template <typename K, typename... A>
-static cudaError_t launch_shares(K kernel, const PagedDecodeArgs& a, int n_slices, int C, size_t smem, cudaStream_t st, const A&... args) {
+static cudaError_t launch_shares(K kernel, const PagedDecodeArgs& a, int n_slices, int C, int warps, size_t smem, cudaStream_t st, const A&... args) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(C > 1 ? n_slices * C : a.ctas)); cfg.blockDim = dim3(kPagedThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.gridDim = dim3((unsigned)(C > 1 ? n_slices * C : a.ctas)); cfg.blockDim = dim3((unsigned)warps * 32); cfg.dynamicSmemBytes = smem; cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -859,18 +861,18 @@ static cudaError_t launch_one(const PagedDecodeArgs& a, cudaStream_t st) {
   const int n_slices = a.p.B * a.p.Hkv, C = paged_cluster(a.p, n_slices, a.ctas);
   cudaError_t e;
   if constexpr (sizeof(T) == 4) {
-    const size_t smem = (size_t)(kPagedWarps * G * D + G * (D + 4)) * 4;
-    e = C > 1 ? launch_shares(paged_decode_kernel<T, D, G, true>, a, n_slices, C, smem, st)
-              : launch_shares(paged_decode_kernel<T, D, G, false>, a, n_slices, C, smem, st);
+    const size_t smem = (size_t)(kPagedWarpsF32 * G * D + G * (D + 4)) * 4;
+    e = C > 1 ? launch_shares(paged_decode_kernel<T, D, G, true>, a, n_slices, C, kPagedWarpsF32, smem, st)
+              : launch_shares(paged_decode_kernel<T, D, G, false>, a, n_slices, C, kPagedWarpsF32, smem, st);
   } else {
-    const size_t smem = (size_t)kPagedWarps * (kPagedStages * 2 * kPagedTile * D * 2 + paged_buffers(G) * G * (D + 8) * 4);
+    const size_t smem = (size_t)paged_warps(G) * (paged_stages(G) * 2 * kPagedTile * D * 2 + paged_buffers(G) * G * (D + 8) * 4);
     PagedMaps maps;
     const int dtype = cuda::std::is_same<T, __half>::value ? D2O_F16 : D2O_BF16;
     const uint64_t rows = (uint64_t)a.p.n_pages * a.p.Hkv << a.p.page_shift;
     if (!encode_rows_2d(&maps.k, dtype, a.p.k, rows, D, kPagedTile) || !encode_rows_2d(&maps.v, dtype, a.p.v, rows, D, kPagedTile))
       return cudaErrorNotSupported;
-    e = C > 1 ? launch_shares(paged_decode_tc_kernel<T, D, G, true>, a, n_slices, C, smem, st, maps)
-              : launch_shares(paged_decode_tc_kernel<T, D, G, false>, a, n_slices, C, smem, st, maps);
+    e = C > 1 ? launch_shares(paged_decode_tc_kernel<T, D, G, true>, a, n_slices, C, paged_warps(G), smem, st, maps)
+              : launch_shares(paged_decode_tc_kernel<T, D, G, false>, a, n_slices, C, paged_warps(G), smem, st, maps);
   }
   if (e != cudaSuccess) return e;
   if (!a.logits) return cudaSuccess;

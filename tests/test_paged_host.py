@@ -90,3 +90,7 @@ def test_binding_refuses_other_tensors():
     for bad, shape, dtype in [(t, (1, 2, 8, 32), torch.float32), (t, t.shape, torch.float16), (t.transpose(1, 2), (1, 8, 2, 64), torch.float32)]:
         with pytest.raises(B.D2OError):
             B._arg(bad, "x", shape, dtype, dev)
+    for view in [(-1, 0), (0, -1), (1 << 31, 0), (0, 1 << 32)]:
+        with pytest.raises(B.D2OError):
+            B._view(*view)
+    assert B._view(0, (1 << 31) - 1) == (0, (1 << 31) - 1)
