@@ -602,6 +602,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     return row0 < 0 ? -1 : row0 + p.in_page(r);
   };
   int asked = 0, ask_row = -1;
+  unsigned long long drop;                                   // read once
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(drop));
   auto copy = [&](long long at, int row) {                   // of the tile at pool row `row`
     if (at >= last) return;
     const int s = asked % STAGES;
@@ -612,8 +614,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
         tc::mbar_expect_tx(&s_full[warp][s], 2 * TILE);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
-          tc::tma_load_2d(to + h * kPagedTile * 128, &maps.k, h * 64, row, &s_full[warp][s]);
-          tc::tma_load_2d(to + TILE + h * kPagedTile * 128, &maps.v, h * 64, row, &s_full[warp][s]);
+          tma_load_2d_hint(to + h * kPagedTile * 128, &maps.k, h * 64, row, &s_full[warp][s], drop);
+          tma_load_2d_hint(to + TILE + h * kPagedTile * 128, &maps.v, h * 64, row, &s_full[warp][s], drop);
         }
       } else {
         tc::mbar_arrive(&s_full[warp][s]);
