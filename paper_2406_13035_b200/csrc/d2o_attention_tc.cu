@@ -38,7 +38,8 @@ __host__ __device__ constexpr int pa_stages(int D) { return D == 128 ? 4 : 8; }
 struct PaMaps { CUtensorMap q, k, v; };
 
 // One item: 256 queries of one (sequence, head).  The last queries see the most keys: items are numbered with those of all heads
-// first, neighbouring heads (which share keys and values) next to one another.
+// first, neighbouring heads (which share keys and values) next to one another.  One CTA of the grid is one item; a CTA that is done takes
+// the place of one that has not started (clusterlaunchcontrol).
 struct PaItem {
   int bh, b, P, q0;
   __device__ __forceinline__ PaItem(const PromptAttentionArgs& a, int i) {
@@ -50,12 +51,6 @@ struct PaItem {
   __device__ __forceinline__ bool empty() const { return q0 >= P; }
   __device__ __forceinline__ bool exists(int t) const { return q0 + t * kPaTile < P; }
 };
-
-// The x-th item of a CTA.  Items come heaviest first, so every second round goes through the CTAs backwards.
-__device__ __forceinline__ int pa_item(int x) {
-  const int c = (int)blockIdx.x, n = (int)gridDim.x;
-  return x * n + (x & 1 ? n - 1 - c : c);
-}
 
 // Does query tile t (first query w) see anything of the key tile at k0?
 __device__ __forceinline__ bool pa_valid(const PromptAttentionArgs& a, int w, int P, int k0) {
@@ -86,7 +81,7 @@ __device__ __forceinline__ void pa_block(const uint32_t (&s)[32], uint32_t (&p)[
 
 template <int D, int FMT>
 __global__ void __launch_bounds__(kPaThreads, 1)
-prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps maps, int n_items) {
+prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps maps) {
   constexpr int KB = D / 64, BLOCK = kPaTile * 128, TILE = KB * BLOCK, STAGES = pa_stages(D);
   constexpr uint32_t IDESC_QK = make_idesc(FMT, kPaTile, kPaTile), IDESC_PV = make_idesc(FMT, kPaTile, D) | kIdescBMn;
   using T = typename cuda::std::conditional<FMT == 0, __half, __nv_bfloat16>::type;
@@ -95,16 +90,19 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   extern __shared__ __align__(1024) unsigned char pa_smem[];
   unsigned char* sQ = pa_smem;                               // [2 tiles][KB][128 rows][128 B]
   unsigned char* sKV = pa_smem + 2 * TILE;                   // [stages][KB][128 rows][128 B]
-  __shared__ unsigned long long q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2][2], o_full[2], o_empty[2], turn[2], all_done[2];
+  __shared__ unsigned long long q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2][2], o_full[2], o_empty[2], turn[2], all_done[2], it_full[2], it_empty[2], answered;
+  __shared__ alignas(16) uint4 s_answer;
+  __shared__ volatile int s_item[2], s_lost;                 // this CTA's current and next item; taken after a wait had run out; -1: none
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_fail;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
+    s_item[0] = s_item[1] = s_lost = -1;
     s_fail = (tc::smem_u32(pa_smem) & 1023u) != 0u;          // swizzled tiles need 1024-byte aligned shared memory
-    tc::mbar_init(&q_full, 1); tc::mbar_init(&q_empty, 2);
+    tc::mbar_init(&q_full, 1); tc::mbar_init(&q_empty, 2); tc::mbar_init(&answered, 1);
     for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&kv_full[s], 1); tc::mbar_init(&kv_empty[s], 2); }
-    for (int t = 0; t < 2; ++t) { tc::mbar_init(&s_full[t], 1); tc::mbar_init(&p_ready[t][0], 4); tc::mbar_init(&p_ready[t][1], 4); tc::mbar_init(&o_full[t], 1); tc::mbar_init(&o_empty[t], 4); tc::mbar_init(&turn[t], 1); tc::mbar_init(&all_done[t], 1); }
+    for (int t = 0; t < 2; ++t) { tc::mbar_init(&it_full[t], 1); tc::mbar_init(&it_empty[t], kPaSoftWarps + 2); tc::mbar_init(&s_full[t], 1); tc::mbar_init(&p_ready[t][0], 4); tc::mbar_init(&p_ready[t][1], 4); tc::mbar_init(&o_full[t], 1); tc::mbar_init(&o_empty[t], 4); tc::mbar_init(&turn[t], 1); tc::mbar_init(&all_done[t], 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
@@ -125,6 +123,14 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   start_dependents();
   wait_for_prior_grid();
   int loads_q = 0, loads_kv = 0;                             // of the producer
+  // The k-th item of this CTA as a warp sees it; -1: no more.
+  auto next_item = [&](int k) {
+    if (!__all_sync(0xffffffffu, wait(&it_full[k & 1], (uint32_t)((k >> 1) & 1)))) return -1;
+    const int i = s_item[k & 1];
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(&it_empty[k & 1]);
+    return i;
+  };
 
   if (warp >= kPaSoftWarps) {
     // 384 threads of 168 registers at launch: 256 of 208 and 128 of 88 from here on
@@ -132,12 +138,17 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
     if (warp == kPaSoftWarps) {
     // ======================================================================= TMA producer
     if (lane == 0) {
-      for (int x = 0, i; (i = pa_item(x)) < n_items && !s_fail; ++x) {
+      int i = (int)blockIdx.x;
+      for (int k = 0;; ++k) {
+        if (k >= 2) (void)wait(&it_empty[k & 1], (uint32_t)(((k >> 1) - 1) & 1));
+        if (s_fail) { s_lost = i; break; }                   // the others run out of time, too
+        s_item[k & 1] = i;
+        tc::mbar_arrive(&it_full[k & 1]);
+        if (i < 0) break;
         const PaItem it(a, i);
-        if (it.empty()) continue;
-        const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
+        const PromptSpan span(it.q0, 2 * kPaTile, max(it.P, it.q0 + 1), kPaTile, a.window, a.n_sink);
         const int q_row = it.bh * a.P + it.q0, k_base = (it.b * a.Hkv + it.bh % a.Hq / (a.Hq / a.Hkv)) * a.P;
-        for (int j = 0; j < 2 * span.tiles; ++j) {           // K, V, K, V ..
+        for (int j = 0; j < (it.empty() ? 0 : 2 * span.tiles); ++j) {      // K, V, K, V ..
           const int s = loads_kv % STAGES;
           if (loads_kv >= STAGES && !wait(&kv_empty[s], (uint32_t)((loads_kv / STAGES - 1) & 1))) break;
           tc::mbar_expect_tx(&kv_full[s], TILE);
@@ -152,6 +163,10 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
             ++loads_q;
           }
         }
+        // Not earlier: the loads are two tiles of keys ahead of the products, which covers the answer's way, and an item asked for at the
+        // beginning of a long one would wait while other CTAs have nothing to do (1200 tokens of 32 heads: 36 us instead of 30).
+        tc::ask_for_cta(&s_answer, &answered);
+        i = tc::mbar_wait(&answered, (uint32_t)(k & 1)) ? tc::cta_answered(&s_answer) : -1;
       }
     }
     __syncwarp();
@@ -161,7 +176,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
     const uint32_t ts = tm_s + t * 128, to = tm_o + t * 128;
     int ring = 0, items = 0, turns = 0, np = 0, no = 0;      // tiles of keys or values, items, turns, weights taken, outputs begun
     auto full = [&](int slot) { return wait(&kv_full[slot % STAGES], (uint32_t)((slot / STAGES) & 1)); };
-    for (int x = 0, i; (i = pa_item(x)) < n_items && !s_fail; ++x) {
+    for (int x = 0, i; (i = next_item(x)) >= 0 && !s_fail; ++x) {
       const PaItem it(a, i);
       if (it.empty()) continue;
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
@@ -236,7 +251,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t ts = tm_s + t * 128 + lanes, to = tm_o + t * 128 + lanes;
     int ns = 0, items = 0;
-    for (int x = 0, i; (i = pa_item(x)) < n_items && !s_fail; ++x) {
+    for (int x = 0, i; (i = next_item(x)) >= 0 && !s_fail; ++x) {
       const PaItem it(a, i);
       if (it.empty() || !it.exists(t)) continue;
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
@@ -344,8 +359,9 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       if (loads_q > 0) (void)tc::mbar_wait(&q_full, (uint32_t)((loads_q - 1) & 1));
       if (a.status) report_error(a.status, D2O_ERR_TIMEOUT, 0xA7710000u | (uint32_t)(blockIdx.x & 0xffff));
     }
-    for (int x = 0, i; x * (int)gridDim.x < n_items; ++x) {   // NaN for all items of this CTA
-      if ((i = pa_item(x)) >= n_items) continue;
+    for (int x = 0; x < 3; ++x) {                            // NaN for the items in hand
+      const int i = x < 2 ? s_item[x] : s_lost;
+      if (i < 0) continue;
       const PaItem it(a, i);
       for (int r = it.q0 + tid; r < min(it.P, it.q0 + 2 * kPaTile); r += kPaThreads) {
         for (int e = 0; e < D; ++e) ((T*)a.out)[((size_t)it.bh * a.P + r) * D + e] = Elem<T>::from_float(NAN);
@@ -357,14 +373,11 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
 
 template <int D, int FMT>
 static cudaError_t launch_one(const PromptAttentionArgs& a, const PaMaps& maps, cudaStream_t st) {
-  int dev = 0, sms = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return cudaGetLastError();
   const size_t smem = (size_t)(2 + pa_stages(D)) * (D / 64) * kPaTile * 128;
   cudaError_t e = cudaFuncSetAttribute(prompt_attention_tc_kernel<D, FMT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const int n_items = a.B * a.Hq * ((a.P + 2 * kPaTile - 1) / (2 * kPaTile));
-  return launch_behind(prompt_attention_tc_kernel<D, FMT>, dim3((unsigned)std::min(n_items, sms)), kPaThreads, smem, st, a, maps, n_items);
+  return launch_behind(prompt_attention_tc_kernel<D, FMT>, dim3((unsigned)n_items), kPaThreads, smem, st, a, maps);
 }
 
 cudaError_t launch_prompt_attention_tc(int dtype, int D, const PromptAttentionArgs& a, cudaStream_t st) {

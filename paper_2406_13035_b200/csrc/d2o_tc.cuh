@@ -157,6 +157,27 @@ __device__ __forceinline__ void mma_commit_one(unsigned long long* bar) {
       "elect.sync x|q, 0xffffffff;\n\t"
       "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)) : "memory");
 }
+// Work from the launch itself: asks for a CTA of this grid that has not started, in whose place this one does its work.  The answer (16
+// bytes) arrives at `answer` and counts on `bar`; no further request once one has been refused.
+__device__ __forceinline__ void ask_for_cta(void* answer, unsigned long long* bar) {
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");            // the answer before has been read
+  mbar_expect_tx(bar, 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];"
+               ::"r"(smem_u32(answer)), "r"(smem_u32(bar)) : "memory");
+}
+// The answer's blockIdx.x; -1: all CTAs have started.
+__device__ __forceinline__ int cta_answered(const void* answer) {
+  uint32_t ok, x;
+  asm volatile(
+      "{\n\t.reg .b128 h;\n\t.reg .pred p;\n\t"
+      "mov.u32 %1, 0;\n\t"
+      "ld.shared.b128 h, [%2];\n\t"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, h;\n\t}"
+      : "=r"(ok), "=&r"(x) : "r"(smem_u32(answer)) : "memory");
+  return ok ? (int)x : -1;
+}
 // Shared-memory matrix descriptor of the same tiles read the other way round (MN-major): the rows of 128 bytes run along N (64
 // elements, the next 64 `block` bytes further), 8 rows of K per group of 1024 bytes.
 __device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t block) {
