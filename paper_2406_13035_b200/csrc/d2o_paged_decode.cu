@@ -28,7 +28,8 @@ constexpr int kPagedWarpsF32 = 8;            // of a CTA
 __host__ __device__ constexpr int paged_warps(int G) { return G <= 4 ? 12 : 8; }
 __host__ __device__ constexpr int paged_stages(int G) { return G <= 4 ? 2 : 3; }
 constexpr int kPagedClusters = 4;            // cluster sizes 1 (none), 2, 4, 8
-constexpr int kPagedMinTiles = 8;            // least share of a CTA: one tile per warp
+constexpr int kPagedMinTiles = 8;            // least share of a CTA where slices are long: a tile for most of its warps
+constexpr int kPagedSnap = 8;
 
 struct PagedDecodeArgs {
   PagedView p;
@@ -39,7 +40,7 @@ struct PagedDecodeArgs {
   int ctas;                                  // CTAs of the first kernel
   uint32_t* done;                            // per slice: parts that are written; zero between launches
   float* lse2;                               // [slices][G] normalisers in the log2 domain (with scores)
-  float* parts;                              // [ctas][2][G][D + 4]: output, maximum, sum, -; 0: the share's first part, 1: its last
+  float* parts;                              // [ctas][2][G][D + 4]: output, maximum, sum, -; 0: of a slice that ends in the share, 1: that goes on
   float* logits;                             // per row of the pools, G logits in the log2 domain (with scores)
 };
 
@@ -47,33 +48,46 @@ struct PagedDecodeArgs {
 __device__ __forceinline__ long long quotient(long long a, long long b) {
   return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// The shares of all tiles: the first `more` CTAs take size + 1 of them, the others, up to `share`, size.
+// The shares of all tiles: the first `more` CTAs take size + 1 of them, the others, up to `share`, size.  A border fewer than kPagedSnap
+// tiles from a border between slices moves there: a part costs more than that many tiles (a CTA has a warp for each), and slices of fewer
+// than twice as many tiles stay whole.
 struct PagedShares {
   long long tot, size;
   int share, more;
   __device__ __forceinline__ PagedShares() {}
-  __device__ __forceinline__ PagedShares(long long tot_, int ctas) : tot(tot_) {
-    share = (int)min((long long)ctas, quotient(tot + kPagedMinTiles - 1, kPagedMinTiles));
+  __device__ __forceinline__ PagedShares(long long tot_, int ctas, int n_slices) : tot(tot_) {
+    share = (int)min((long long)ctas, max(quotient(tot + kPagedMinTiles - 1, kPagedMinTiles), min((long long)n_slices, tot)));
     size = share ? quotient(tot, share) : 0;
     more = (int)(tot - size * share);
   }
-  __device__ __forceinline__ long long begin(int c) const { return c * size + min(c, more); }
+  __device__ __forceinline__ long long border(int c) const { return c * size + min(c, more); }       // before it moves
   __device__ __forceinline__ int of_tile(long long tile) const {
     const long long head = more * (size + 1);
     return tile < head ? (int)quotient(tile, size + 1) : more + (int)quotient(tile - head, size);
   }
+  static __device__ __forceinline__ long long snap(long long x, long long before, int tiles) {         // a border in that slice
+    return x - before < kPagedSnap ? before : before + tiles - x < kPagedSnap ? before + tiles : x;
+  }
+  // first and last share with tiles of a slice that more than one has: those that end or begin at its unmoved borders
+  __device__ __forceinline__ int first_of(long long before) const { return of_tile(before + kPagedSnap - 1); }
+  __device__ __forceinline__ int last_of(long long before, int tiles) const { return of_tile(before + tiles - kPagedSnap); }
 };
 
-// Where this CTA begins: tiles before its first slice, and that slice.  Every CTA adds up the tiles of all slices: a thread
+// A CTA's share: tiles first .. last, and the slice in which it begins.  Every CTA adds up the tiles of all slices: a thread
 // those of consecutive slices, then a scan over the block.
 struct PagedStart {
   PagedShares shares;
+  long long first, last;
   long long before;                          // tiles ahead of `slice`
   int slice;                                 // -1: no share
   int n;                                     // rows that it holds
 };
+struct PagedStartShared {
+  long long sum[16], border[2], before;
+  int slice, n;
+};
 template <int NW, typename F>
-__device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int c, long long* s_scan /* [warps + 1] */, int* s_found, F&& short_table) {
+__device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int c, PagedStartShared& sh, F&& short_table) {
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n_slices = p.B * p.Hkv, per = (n_slices + (NW * 32) - 1) / (NW * 32);
@@ -87,38 +101,46 @@ __device__ __forceinline__ PagedStart paged_start(const PagedDecodeArgs& a, int 
   long long inc = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const long long t = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += t; }
-  if (lane == 31) s_scan[warp] = inc;
+  if (lane == 31) sh.sum[warp] = inc;
   __syncthreads();
   long long base = 0, tot = 0;
 #pragma unroll
-  for (int w = 0; w < NW; ++w) { if (w < warp) base += s_scan[w]; tot += s_scan[w]; }
+  for (int w = 0; w < NW; ++w) { if (w < warp) base += sh.sum[w]; tot += sh.sum[w]; }
   PagedStart r;
-  r.shares = PagedShares(tot, a.ctas); r.slice = -1; r.before = 0; r.n = 0;
-  const long long first = c < r.shares.share ? r.shares.begin(c) : tot;
-  long long at = base + inc - mine;
-  if (first >= at && first < at + mine) {                    // one thread
-    int s = s0;
-    for (;; ++s) {
-      const int tiles = PagedSpan(p.len[s], p.reach(), a.window, a.n_sink).tiles;
-      if (first < at + tiles) break;
-      at += tiles;
+  r.shares = PagedShares(tot, a.ctas, n_slices); r.slice = -1;
+  if (c >= r.shares.share) return r;
+  const long long at0 = base + inc - mine;
+  for (int e = 0; e < 2; ++e) {                              // its two borders
+    const long long x = r.shares.border(c + e);
+    if (x >= at0 && x < at0 + mine) {                        // one thread
+      long long at = at0;
+      int s = s0, n, tiles;
+      for (;; ++s) {
+        n = p.len[s];
+        tiles = PagedSpan(n, p.reach(), a.window, a.n_sink).tiles;
+        if (x < at + tiles) break;
+        at += tiles;
+      }
+      sh.border[e] = PagedShares::snap(x, at, tiles);
+      if (e == 0) { sh.slice = s; sh.n = n; sh.before = at; }
     }
-    s_found[0] = s; s_found[1] = p.len[s]; s_scan[NW] = at;
+    if (x == tot && tid == 0) sh.border[e] = tot;
   }
   __syncthreads();
-  if (c < r.shares.share) { r.slice = s_found[0]; r.n = s_found[1]; r.before = s_scan[NW]; }
+  r.first = sh.border[0]; r.last = sh.border[1]; r.before = sh.before; r.n = sh.n;
+  if (r.first < r.last) r.slice = sh.slice;
   return r;
 }
 
 // The share of a CTA in a cluster per slice: its first tile, and behind its last one, of the slice's.  -1: nothing to do.
 template <typename F>
-__device__ __forceinline__ PagedStart cluster_start(const PagedDecodeArgs& a, int& first, int& last, F&& short_table) {
+__device__ __forceinline__ PagedStart cluster_start(const PagedDecodeArgs& a, F&& short_table) {
   const cg::cluster_group cluster = cg::this_cluster();
   const int C = (int)cluster.num_blocks(), r = (int)cluster.block_rank(), sl = (int)blockIdx.x / C, n = a.p.len[sl];
   const PagedSpan span(n, a.p.reach(), a.window, a.n_sink);
-  first = span.tiles * r / C; last = span.tiles * (r + 1) / C;
   if (n >= a.p.reach() && r == 0 && threadIdx.x == 0) short_table(sl);
   PagedStart s;
+  s.first = span.tiles * r / C; s.last = span.tiles * (r + 1) / C;
   s.slice = span.t < 0 ? -1 : sl; s.before = 0; s.n = n;
   return s;
 }
@@ -131,14 +153,14 @@ __device__ __forceinline__ void short_table_output(const PagedDecodeArgs& a, int
   for (int i = 0; i < G * D; ++i) out[i] = Elem<T>::from_float(NAN);
 }
 
-// Joins the parts c0 .. c1 of a slice (part `slot` of the first share, the first part of the others).  NW / G warps per head,
+// Joins the parts that the shares c0 .. c1 have of a slice (in c1, where it ends, place 0; in those that it goes on behind, place 1).  NW / G warps per head,
 // each every so many parts, whose results are added in shared memory: the order is that of the shares whatever CTA does it.
 template <typename T, int D, int G, int NW>
-__device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int c0, int c1, int slot, float4* s_acc /* [warps][D / 4] */) {
+__device__ __forceinline__ void join_parts(const PagedDecodeArgs& a, int sl, int c0, int c1, float4* s_acc /* [warps][D / 4] */) {
   constexpr int LPR = D / 4, RPW = 32 / LPR, W = NW / G, STEP = W * RPW;        // lanes per row of D floats, rows of a warp, warps per head
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = min(warp / W, G - 1), sub = warp % W, lig = lane % LPR;
   const bool spare = warp >= W * G;                          // more warps than heads take
-  auto part = [&](int c) { return a.parts + (((size_t)c * 2 + (c == c0 ? slot : 0)) * G + g) * (D + 4); };
+  auto part = [&](int c) { return a.parts + (((size_t)c * 2 + (c < c1 ? 1 : 0)) * G + g) * (D + 4); };
   // the first outputs on their way beside the maxima
   constexpr int AHEAD = 2;
   float4 ahead[AHEAD];
@@ -291,25 +313,24 @@ __device__ __forceinline__ void join_cluster(const PagedDecodeArgs& a, int sl, f
 template <typename T, int D, int G, int NW>
 __device__ __forceinline__ void close_parts(const PagedDecodeArgs& a, const PagedStart& start, const PagedOpen& open, float* red, int4* s_join /* [2] */) {
   if (open.n == 0) return;                                   // the caller's barrier lies behind the last part
-  // A slice's parts are those of all shares that hold tiles of it; it is a share's second part unless it begins the share.  Thread x
-  // looks after part x.
+  // thread x looks after part x
   if (threadIdx.x < open.n) {
     const int x = threadIdx.x, sl = x ? open.sl[1] : open.sl[0], tiles = x ? open.tiles[1] : open.tiles[0];
     const long long first = x ? open.before[1] : open.before[0];
-    const int c0 = start.shares.of_tile(first), c1 = start.shares.of_tile(first + tiles - 1);
+    const int c0 = start.shares.first_of(first), c1 = start.shares.last_of(first, tiles);
     uint32_t before;
     // the CTA's stores, ordered ahead of this thread by the barrier, become visible with the count; with the last count the others' are
     asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.done + sl) : "memory");
     const bool all = before == (uint32_t)(c1 - c0);
     if (all) a.done[sl] = 0u;                                // for the next launch
-    s_join[x] = make_int4(all ? sl : -1, c0, c1, first == start.shares.begin(c0) ? 0 : 1);
+    s_join[x] = make_int4(all ? sl : -1, c0, c1, 0);
   }
   __syncthreads();
 #pragma unroll 1                                             // code that is run once comes from far: half of it
   for (int x = 0; x < open.n; ++x) {
     const int4 j = s_join[x];
     if (j.x < 0) continue;
-    join_parts<T, D, G, NW>(a, j.x, j.y, j.z, j.w, reinterpret_cast<float4*>(red));
+    join_parts<T, D, G, NW>(a, j.x, j.y, j.z, reinterpret_cast<float4*>(red));
     __syncthreads();                                         // before the exchange area is written again
   }
 }
@@ -322,24 +343,22 @@ paged_decode_kernel(PagedDecodeArgs a) {
   constexpr int EPV = Elem<T>::kPerVec, LPR = D / EPV, RPW = 32 / LPR, U = kPagedTile / RPW, QL = LPR / 4;
   extern __shared__ __align__(16) float red[];               // [warps][G][D]
   __shared__ float s_m[kPagedWarpsF32][G], s_l[kPagedWarpsF32][G];
-  __shared__ long long s_scan[kPagedWarpsF32 + 1];
-  __shared__ int s_found[2];
+  __shared__ PagedStartShared s_start;
   __shared__ int4 s_join[2];
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int grp = lane / LPR, lig = lane % LPR, c = blockIdx.x;
   auto short_table = [&](int sl) { short_table_output<T, D, G>(a, sl); };
-  int c_first = 0, c_last = 0;
-  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start<kPagedWarpsF32>(a, c, s_scan, s_found, short_table);
+  const PagedStart start = CL ? cluster_start(a, short_table) : paged_start<kPagedWarpsF32>(a, c, s_start, short_table);
   if (start.slice < 0) return;
-  const long long first = CL ? c_first : start.shares.begin(c), last = CL ? c_last : start.shares.begin(c + 1);
+  const long long first = start.first, last = start.last;
   float* swap = red + kPagedWarpsF32 * G * D;                   // [G][D + 4], clusters
   long long before = start.before;
   int sl = start.slice;
   PagedOpen open;
   for (long long at = first; at < last; ++sl) {
     const PagedSpan span(p.len[sl], p.reach(), a.window, a.n_sink);
-    if (span.tiles == 0) continue;
+    if (at >= before + span.tiles) { before += span.tiles; continue; }       // absent, or the share begins behind it
     const int b = sl / p.Hkv, h = sl % p.Hkv;
     const int i0 = (int)(at - before), i1 = (int)min((long long)span.tiles, last - before);      // this part: tiles i0 .. i1 of the slice
     const T* q_in = (const T*)a.q + ((size_t)b * p.Hq + (size_t)h * G) * D;
@@ -461,7 +480,7 @@ paged_decode_kernel(PagedDecodeArgs a) {
       }
     }
     __syncthreads();
-    finish_part<T, D, G, D, CL>(a, start, open, swap, at == first ? 0 : 1, sl, i0, i1, span, before, red, &s_m[0][0], &s_l[0][0], G);
+    finish_part<T, D, G, D, CL>(a, start, open, swap, i1 < span.tiles ? 1 : 0, sl, i0, i1, span, before, red, &s_m[0][0], &s_l[0][0], G);
     __syncthreads();                                         // before the exchange area is written again
     at = before + i1;
     before += span.tiles;
@@ -573,8 +592,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   __shared__ unsigned long long s_full[WARPS][STAGES], s_written[BUFS], s_free[BUFS];
   __shared__ int s_row[WARPS][STAGES];           // pool row of the stage's tile; -1: bad page
   __shared__ float s_m[BUFS][WARPS][G + G % 2], s_l[BUFS][WARPS][G + G % 2];
-  __shared__ long long s_scan[WARPS + 1];
-  __shared__ int s_found[2];
+  __shared__ PagedStartShared s_start;
   __shared__ int4 s_join[2];
   const PagedView& p = a.p;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3, c = blockIdx.x;
@@ -588,10 +606,9 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   __syncwarp();
   asm volatile("fence.proxy.async.global;" ::: "memory");    // rows that kernels ahead wrote with ordinary stores are read by copies
   auto short_table = [&](int sl) { short_table_output<T, D, G>(a, sl); };
-  int c_first = 0, c_last = 0;
-  const PagedStart start = CL ? cluster_start(a, c_first, c_last, short_table) : paged_start<WARPS>(a, c, s_scan, s_found, short_table);
+  const PagedStart start = CL ? cluster_start(a, short_table) : paged_start<WARPS>(a, c, s_start, short_table);
   if (start.slice < 0) return;
-  const long long first = CL ? c_first : start.shares.begin(c), last = CL ? c_last : start.shares.begin(c + 1);
+  const long long first = start.first, last = start.last;
   unsigned char* my_ring = ring + (size_t)warp * STAGES * 2 * TILE;
 
   // ---- requests: the cursor is one tile ahead of them, its page number on the way
@@ -780,7 +797,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     if (warp == parts % WARPS) {
       if (!lost && !tc::mbar_wait(&s_written[buf], phase)) lost = true;
       if (CL && lost) land();                                // the part goes to the ring's place
-      float* to = CL ? reinterpret_cast<float*>(paged_smem) : a.parts + ((size_t)c * 2 + (cur.at == first ? 0 : 1)) * G * (D + 4);
+      float* to = CL ? reinterpret_cast<float*>(paged_smem) : a.parts + ((size_t)c * 2 + (end < cur.before + span.tiles ? 1 : 0)) * G * (D + 4);
       combine_warps<T, D, G, LD>(a, sl, b, h, whole, to, red + (size_t)buf * WARPS * G * LD, &s_m[buf][0][0], &s_l[buf][0][0]);
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&s_free[buf]);
