@@ -280,6 +280,96 @@ def test_decode_offsets_past_32_bits(cuda_device):
     c.check()
 
 
+# ---------------------------------------------------------------------------------------------- many, at once, and with one scratch
+def _batch(seed, b, hkv, G, d, dtype, page, held, scored=False):
+    """A cache made on the GPU, lengths 0 .. held; returns it with its tensors and a function for the float64 output of one slice."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    per = held // page + 1
+    n_pages = b * per + 1
+    table = torch.randperm(n_pages, generator=g, device="cuda")[: b * per].view(b, per).to(torch.int32)
+    kp, vp = (torch.randn(n_pages, hkv, page, d, generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    length = torch.randint(0, held + 1, (b, hkv), generator=g, device="cuda", dtype=torch.int32)
+    q, k, v = (torch.randn(b, h, d, generator=g, device="cuda").to(DT[dtype]) for h in (hkv * G, hkv, hkv))
+    pos = torch.zeros(n_pages, hkv, page, dtype=torch.int32, device="cuda") if scored else None
+    score = torch.zeros(n_pages, hkv, page, device="cuda") if scored else None
+    c = B.D2OPagedCache(kp, vp, table, length, n_q_heads=hkv * G, pos=pos, score=score)
+
+    def check(out, slices):
+        for i, h in slices:
+            n = int(length[i, h])
+            rows = lambda pool: pool[table[i].long(), h].flatten(0, 1)[: n + 1].double()
+            K, V, Q = rows(kp), rows(vp), q[i, h * G:(h + 1) * G].double()
+            assert torch.equal(K[n], k[i, h].double()) and torch.equal(V[n], v[i, h].double())
+            p = torch.softmax(Q @ K.T / math.sqrt(d), -1)
+            w = 32 * 2.0 ** -24 * float((Q.abs() @ K.abs().T).max()) / math.sqrt(d) + 2.0 ** -20
+            e, ref = (w + (2.0 ** -16 if dtype == "bf16" else 0)) * (p @ V.abs()), p @ V
+            o = out[i, h * G:(h + 1) * G].double()
+            assert bool((((ref - e).to(DT[dtype]).double() <= o) & (o <= (ref + e).to(DT[dtype]).double())).all()), (i, h, n)
+    return c, q, k, v, torch.full_like(q, NAN), check
+
+
+@pytest.mark.parametrize("b,hkv,G,d,dtype,held", [(8191, 8, 1, 64, "f16", 15), (8191, 8, 1, 64, "f32", 15), (600, 8, 2, 128, "bf16", 100), (40, 8, 4, 128, "bf16", 3000),
+                                                  (40, 8, 8, 128, "f16", 900), (9, 2, 8, 64, "f32", 2500), (150, 1, 1, 128, "bf16", 700)])
+def test_decode_many(cuda_device, b, hkv, G, d, dtype, held):
+    """The most slices, more slices than SMs of lengths around the borders of the shares, every group size."""
+    c, q, k, v, out, check = _batch(b + held, b, hkv, G, d, dtype, 16, held)
+    c.d2o_paged_decode_step(q, k, v, out)
+    assert bool(torch.isfinite(out.float()).all())
+    g = torch.Generator().manual_seed(1)
+    check(out, [(int(i), int(i) % hkv) for i in torch.randint(0, b, (60,), generator=g)] + [(0, 0), (b - 1, hkv - 1)])
+    again = torch.empty_like(out)
+    c.d2o_paged_decode_step(q, k, v, again)
+    assert torch.equal(out, again)
+    c.check()
+    zero = c._scratch[0] - c.scratch.data_ptr()
+    assert not c.scratch[zero:zero + B.PAGED_ZERO_BYTES].any()                 # as every call leaves them
+
+
+def test_streams_at_once(cuda_device):
+    """Steps on two caches, an eviction on a third and a prompt's attention, on four streams at the same time, many times over: the bits
+    of the same calls one after another."""
+    a = _batch(1, 20, 8, 4, 128, "bf16", 16, 1500)
+    b = _batch(2, 3, 8, 1, 64, "f32", 32, 4000)
+    Q, K, V = (torch.randn(2, h, 500, 128, device="cuda").half() for h in (8, 2, 2))
+    want = []
+    for c, q, k, v, out, _ in (a, b):
+        c.d2o_paged_decode_step(q, k, v, out, window=700, n_sink=3)
+        want.append(out.clone())
+    o = torch.empty_like(Q)
+    B.d2o_prompt_attention(Q, K, V, o, window=100, n_sink=2)
+    want.append(o.clone())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(20):
+        for t in (a[4], b[4], o):
+            t.zero_()
+        torch.cuda.synchronize()
+        for st, x in zip(streams, (a, b)):
+            with torch.cuda.stream(st):
+                for _ in range(3):
+                    x[0].d2o_paged_decode_step(x[1], x[2], x[3], x[4], window=700, n_sink=3)
+        with torch.cuda.stream(streams[2]):
+            for _ in range(3):
+                B.d2o_prompt_attention(Q, K, V, o, window=100, n_sink=2)
+        torch.cuda.synchronize()
+        assert torch.equal(a[4], want[0]) and torch.equal(b[4], want[1]) and torch.equal(o, want[2])
+
+
+def test_one_scratch_for_several_caches(cuda_device):
+    """Caches of other shapes in turn on one scratch, as large as the largest asks for."""
+    caches = [_batch(i, b, hkv, G, d, dt, 16, held, True) for i, (b, hkv, G, d, dt, held) in enumerate(
+        [(30, 8, 4, 128, "bf16", 900), (1, 1, 1, 64, "f32", 20000), (700, 2, 2, 64, "f16", 40)])]
+    big = max(caches, key=lambda x: x[0]._scratch[1])[0]
+    for _ in range(2):
+        for c, q, k, v, out, check in caches:
+            c._scratch = big._scratch
+            c.d2o_paged_decode_step(q, k, v, out)
+            b, hkv = c.tensors[3].shape
+            check(out, [(i, i % hkv) for i in range(0, b, max(1, b // 8))])
+            c.d2o_paged_evict((c.tensors[3] + 1).contiguous(), torch.full((b,), 30000, dtype=torch.int32, device="cuda"))     # nothing to do
+            c.check()
+
+
 # ---------------------------------------------------------------------------------------------- evict
 @pytest.mark.parametrize("b,hq,hkv,d,dtype,page,held,budget,window,sinks", [
     (1, 1, 1, 64, "f32", 16, [1], [0], 0, 0), (1, 1, 1, 64, "f32", 16, [2], [1], 0, 0), (1, 2, 2, 128, "bf16", 16, [40], [39], 4, 1),
