@@ -103,6 +103,7 @@ constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictKeys = 12288;            // rows of a CTA whose keys stay in shared memory
 constexpr int kEvictMaxCluster = 16;
+constexpr int kEvictMinRows = 1024;          // rows of a full table per CTA of a cluster
 constexpr int kEvictMoves = 4;               // moves of a group of lanes in flight
 constexpr int kEvictFew = kEvictThreads;     // rows in question that are ranked one by one instead of by further rounds
 
@@ -404,8 +405,12 @@ cudaError_t launch_paged_evict(const PagedView& p, int dtype, int D, const int32
   const int n_slices = p.B * p.Hkv;
   const PagedScratch s(n_slices, p.Hq / p.Hkv, D, (size_t)p.n_pages * p.Hkv << p.page_shift, true);
   const EvictArgs a = {p, budgets, next_pos, reinterpret_cast<int2*>(scratch + s.rows), n_sink, window};
-  int C = 1;                                                 // one CTA per SM
-  while (2 * C <= kEvictMaxCluster && (long)n_slices * 2 * C <= sms) C *= 2;
+  // One CTA per SM, as long as the table could hold 1024 rows for each of a cluster (the rows are known on the device only).  us with the
+  // restoring copy, 8 slices: of 100 rows 7.2 (one CTA) against 15.7 (sixteen), of 1100 10.4 / 16.4, of 5300 18.4 (four) against 29.0 (one)
+  // and 19.3 (sixteen), of 9000 19.6 (eight) / 32.9 / 22.0.
+  int C = 1;
+  const long long reach = (long long)p.max_pages << p.page_shift;
+  while (2 * C <= kEvictMaxCluster && (long)n_slices * 2 * C <= sms && reach >= (long long)kEvictMinRows * 2 * C) C *= 2;
   const int rowb = D * (dtype == D2O_F32 ? 4 : 2);
   return rowb == 128 ? launch_evict<128>(a, n_slices, C, st) : rowb == 256 ? launch_evict<256>(a, n_slices, C, st)
                                                                            : launch_evict<512>(a, n_slices, C, st);
