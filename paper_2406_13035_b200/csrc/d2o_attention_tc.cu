@@ -14,11 +14,13 @@
 // domain): O in tensor memory is then rescaled by the softmax warps themselves.  The product before it has finished by then: the
 // commit that announces a new S covers every product issued ahead of it.
 //
+// What bounds it: neither the tensor cores (57 % busy) nor the exponentials (57 %) but a query tile's chain from S to the next S, 3000 - 3200
+// cycles against 2050 of products for both tiles; under load the power cap.  us: 32 / 8 heads of 32768 tokens under a window of 4096, bf16, 1800 cool and
+// 2190 warm (1.15 and 0.94 PFLOP/s); four ragged prompts of up to 6001 tokens 450 - 505; 32 heads of 1200 tokens 28.
+//
 // Rounding: weights to the input type for their product (relative half step 2^-9 bf16, 2^-12 fp16; the largest is 2^0 to 2^8, and
 // the errors of many keys average out); their sum and lse from the unrounded ones; S, O and all sums are fp32.
 #include <math.h>
-
-#include <algorithm>
 
 #include <cuda/std/type_traits>
 

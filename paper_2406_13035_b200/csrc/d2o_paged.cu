@@ -26,8 +26,8 @@ struct AppendArgs {
   int n_rows;
 };
 
-// A copy: bound by HBM, each byte read and written once.  A group of lanes takes one row's 16-byte pieces of K and V, four rows
-// in flight.
+// A copy: bound by HBM, each byte read and written once (four prompts of 4096 tokens, 32 heads, fp16, with scores: 543 MB in 85 us, 6.4 TB/s).
+// A group of lanes takes one row's 16-byte pieces of K and V, four rows in flight.
 template <int ROWB>
 __global__ void __launch_bounds__(kAppendThreads)
 append_kernel(AppendArgs a) {
@@ -137,7 +137,8 @@ struct EvictExchange {                       // read by the other CTAs of the cl
 // (every warp counts its own consecutive rows, one scan, every warp numbers them), form the moves; as many of one as of the other, and
 // sources and targets do not overlap, so that all moves run at once.  (4) The moves, divided over the cluster, several rows of a
 // group of lanes in flight.  What costs are the dependent steps.  us, counting lane by lane, numbering by block scans twice, one row in
-// flight, clusters of at most eight: 8 slices of 32768 rows to 6554 63, 256 slices of 2064 rows to 2048 31.
+// flight, clusters of at most eight / so (with the copy that restores the scores): 8 slices of 32768 rows to 6554 63 / 34 (selection 15, moves
+// 9 at 5 TB/s), 256 slices of 2064 rows to 2048 31 / 16.
 template <int ROWB, bool CL>
 __global__ void __launch_bounds__(kEvictThreads, 2)
 evict_kernel(EvictArgs a) {
