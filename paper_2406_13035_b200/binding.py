@@ -399,14 +399,14 @@ def _need(ok: bool, what: str):
         raise D2OError(1, what)
 
 
-def _arg(t: Optional[torch.Tensor], name: str, shape, dtype, device) -> Optional[int]:
-    """The address of a tensor that has to be contiguous, of this shape and type and on this device (None: NULL)."""
+def _arg(t: Optional[torch.Tensor], name: str, shape, dtype, index: int) -> Optional[int]:
+    """The address of a tensor that has to be contiguous, of this shape and type and on this GPU (None: NULL)."""
     if t is None:
         return None
-    if t.shape == shape and t.dtype is dtype and t.device == device and t.is_contiguous():
+    if t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == index:
         return t.data_ptr()
-    raise D2OError(1, f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is needed, got "
-                      f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    raise D2OError(1, f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on GPU {index} is needed, got "
+                      f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
 def _view(window: int, n_sink: int):
@@ -415,12 +415,14 @@ def _view(window: int, n_sink: int):
     return window, n_sink
 
 
-def _call(device: torch.device, what: str, fn, *args):
+def _call(index: int, what: str, fn, *args):
     """fn(*args, stream) with the tensors' device current: their stream is that device's current one."""
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream()), what)
+    if index == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(index) if _raw_stream else _stream())
+        if status:
+            _check(status, what)
         return
-    with torch.cuda.device(device):
+    with torch.cuda.device(index):
         _check(fn(*args, _stream()), what)
 
 
@@ -433,7 +435,7 @@ def d2o_prompt_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out:
     there is no window); lens int32 [B], status int32 [2], all on the GPU."""
     _need(Q.dim() == 4 and K.dim() == 4 and Q.dtype in DTYPE_CODE and Q.is_cuda, "Q, K: [B, H, P, d] on the GPU")
     b, hq, n, d = Q.shape
-    hkv, dev = K.shape[1], Q.device
+    hkv, dev = K.shape[1], Q.get_device()
     _call(dev, "d2o_prompt_attention", load_library().d2o_prompt_attention, DTYPE_CODE[Q.dtype], d, b, hq, hkv, n, *_view(window, n_sink),
           _arg(Q, "Q", (b, hq, n, d), Q.dtype, dev), _arg(K, "K", (b, hkv, n, d), Q.dtype, dev),
           _arg(V, "V", (b, hkv, n, d), Q.dtype, dev), _arg(lens, "lens", (b,), torch.int32, dev),
@@ -456,15 +458,16 @@ class D2OPagedCache:
         _need(page_table.dim() == 2, "page_table: [B, max_pages]")
         n_pages, hkv, page, d = k_pages.shape
         b, max_pages = page_table.shape
-        dev = self.device = k_pages.device
+        dev = k_pages.device
+        self.device, self.index = dev, k_pages.get_device()
         self.dtype, self.shape = k_pages.dtype, (b, n_q_heads, hkv, d)
         self.status = torch.zeros(2, dtype=torch.int32, device=dev)
         self.tensors = (k_pages, v_pages, page_table, length, pos, score)
         self.cache = D2OPaged(
             DTYPE_CODE[k_pages.dtype], d, b, n_q_heads, hkv, page, n_pages, max_pages,
-            _arg(k_pages, "k_pages", k_pages.shape, k_pages.dtype, dev), _arg(v_pages, "v_pages", k_pages.shape, k_pages.dtype, dev),
-            _arg(pos, "pos", (n_pages, hkv, page), torch.int32, dev), _arg(score, "score", (n_pages, hkv, page), torch.float32, dev),
-            _arg(page_table, "page_table", (b, max_pages), torch.int32, dev), _arg(length, "length", (b, hkv), torch.int32, dev),
+            _arg(k_pages, "k_pages", k_pages.shape, k_pages.dtype, self.index), _arg(v_pages, "v_pages", k_pages.shape, k_pages.dtype, self.index),
+            _arg(pos, "pos", (n_pages, hkv, page), torch.int32, self.index), _arg(score, "score", (n_pages, hkv, page), torch.float32, self.index),
+            _arg(page_table, "page_table", (b, max_pages), torch.int32, self.index), _arg(length, "length", (b, hkv), torch.int32, self.index),
             self.status.data_ptr())
         n = C.c_size_t()
         _check(self.lib.d2o_paged_workspace_size(C.byref(self.cache), C.byref(n)), "d2o_paged_workspace_size")
@@ -477,26 +480,28 @@ class D2OPagedCache:
                          first_pos: Optional[torch.Tensor] = None, colsum: Optional[torch.Tensor] = None):
         b, hq, hkv, d = self.shape
         _need(K.dim() == 4, "K, V: [B, Hkv, n_rows, d]")
-        n, dev, i32 = K.shape[2], self.device, torch.int32
-        _call(dev, "d2o_paged_append", self.lib.d2o_paged_append, self._ref, n,
-              _arg(K, "K", (b, hkv, n, d), self.dtype, dev), _arg(V, "V", (b, hkv, n, d), self.dtype, dev),
-              _arg(lens, "lens", (b,), i32, dev), _arg(first_pos, "first_pos", (b,), i32, dev),
-              _arg(colsum, "colsum", (b, hq, n), torch.float32, dev))
+        n, x, dt = K.shape[2], self.index, self.dtype
+        rows = (b, hkv, n, d)
+        _call(x, "d2o_paged_append", self.lib.d2o_paged_append, self._ref, n, _arg(K, "K", rows, dt, x), _arg(V, "V", rows, dt, x),
+              _arg(lens, "lens", (b,), torch.int32, x), _arg(first_pos, "first_pos", (b,), torch.int32, x),
+              _arg(colsum, "colsum", (b, hq, n), torch.float32, x))
 
     def d2o_paged_decode_step(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, *,
                               positions: Optional[torch.Tensor] = None, window: int = 0, n_sink: int = 0):
         b, hq, hkv, d = self.shape
-        dev, dt = self.device, self.dtype
-        _call(dev, "d2o_paged_decode_step", self.lib.d2o_paged_decode_step, self._ref, *_view(window, n_sink),
-              _arg(q, "q", (b, hq, d), dt, dev), _arg(k, "k", (b, hkv, d), dt, dev), _arg(v, "v", (b, hkv, d), dt, dev),
-              _arg(positions, "positions", (b,), torch.int32, dev), _arg(out, "out", (b, hq, d), dt, dev), *self._scratch)
+        x, dt, heads, kv = self.index, self.dtype, (b, hq, d), (b, hkv, d)
+        if window or n_sink:
+            _view(window, n_sink)
+        _call(x, "d2o_paged_decode_step", self.lib.d2o_paged_decode_step, self._ref, window, n_sink, _arg(q, "q", heads, dt, x),
+              _arg(k, "k", kv, dt, x), _arg(v, "v", kv, dt, x), _arg(positions, "positions", (b,), torch.int32, x),
+              _arg(out, "out", heads, dt, x), *self._scratch)
 
     def d2o_paged_evict(self, budgets: torch.Tensor, next_pos: torch.Tensor, *, n_sink: int = 0, window: int = 0):
         b, _, hkv, _ = self.shape
-        window, n_sink = _view(window, n_sink)
-        _call(self.device, "d2o_paged_evict", self.lib.d2o_paged_evict, self._ref,
-              _arg(budgets, "budgets", (b, hkv), torch.int32, self.device), _arg(next_pos, "next_pos", (b,), torch.int32, self.device),
-              n_sink, window, *self._scratch)
+        _view(window, n_sink)
+        x = self.index
+        _call(x, "d2o_paged_evict", self.lib.d2o_paged_evict, self._ref, _arg(budgets, "budgets", (b, hkv), torch.int32, x),
+              _arg(next_pos, "next_pos", (b,), torch.int32, x), n_sink, window, *self._scratch)
 
     def check(self):
         """Raises if a call on this cache has met a bad length or page number since the last check.  Synchronises."""

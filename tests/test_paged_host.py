@@ -85,9 +85,10 @@ def test_binding_refuses_other_tensors():
         B.d2o_prompt_attention(t, t, t, t)                                    # not on a GPU
     with pytest.raises(B.D2OError):
         B.D2OPagedCache(t, t, torch.zeros(1, 1, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32), n_q_heads=2)
-    dev = t.device
-    assert B._arg(None, "x", (1,), torch.float32, dev) is None
-    for bad, shape, dtype in [(t, (1, 2, 8, 32), torch.float32), (t, t.shape, torch.float16), (t.transpose(1, 2), (1, 8, 2, 64), torch.float32)]:
+    cpu = t.get_device()
+    assert B._arg(None, "x", (1,), torch.float32, cpu) is None and B._arg(t, "x", t.shape, torch.float32, cpu) == t.data_ptr()
+    for bad, shape, dtype, dev in [(t, (1, 2, 8, 32), torch.float32, cpu), (t, t.shape, torch.float16, cpu), (t, t.shape, torch.float32, 0),
+                                   (t.transpose(1, 2), (1, 8, 2, 64), torch.float32, cpu)]:
         with pytest.raises(B.D2OError):
             B._arg(bad, "x", shape, dtype, dev)
     for view in [(-1, 0), (0, -1), (1 << 31, 0), (0, 1 << 32)]:
