@@ -858,10 +858,13 @@ score_kernel(PagedDecodeArgs a) {
 // CTAs per slice of a call whose slices get a cluster each, 1: shares of all tiles.  A cluster joins its parts through distributed shared
 // memory, in about a microsecond where counters and parts in global memory take five; but it knows no other slice, and one that is much
 // longer than the rest is left with its own CTAs.  So: calls whose slices get at least two CTAs each with one CTA per SM, up to eight
-// (the portable size), as long as what the table can hold gives a CTA at most 64 tiles (16-bit rows of d = 128: 512 KB, 10 us).
+// (the portable size; for up to three quarters of the SMs, because sixteen clusters of eight are not resident at once), as long as what
+// the table can hold gives a CTA at most 64 tiles (16-bit rows of d = 128: 512 KB, 10 us).  us, shares / clusters, 8 KV heads, d = 128, bf16: one
+// sequence of 3000 rows 11.7 / 9.0, of 7000 17.0 / 12.6, two of 3000 15.1 / 11.1 (16.9 with eight CTAs each), four of 3000 16.8 / 11.6; nine
+// ragged ones of up to 3500 (beyond the bound) 16.5 / 18.2.
 static int paged_cluster(const PagedView& p, int n_slices, int sms) {
   int C = 1;
-  while (2 * C <= 1 << (kPagedClusters - 1) && (long)n_slices * 2 * C <= sms) C *= 2;
+  while (2 * C <= 1 << (kPagedClusters - 1) && (long)n_slices * 2 * C <= (2 * C < 8 ? sms : sms * 3 / 4)) C *= 2;
   return ((long long)p.max_pages << p.page_shift) <= 64ll * kPagedTile * C ? C : 1;
 }
 
