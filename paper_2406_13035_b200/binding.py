@@ -449,7 +449,10 @@ class D2OPagedCache:
 
     k_pages, v_pages [n_pages, Hkv, page_size, d]; page_table int32 [B, max_pages]; length int32 [B, Hkv], rows held
     (negative: no such sequence); pos int32 and score float32 [n_pages, Hkv, page_size], both or neither.  The caller
-    changes the contents of page_table and length between the calls, in place; the library never does."""
+    changes the contents of page_table and length between the calls, in place; the library never does.
+
+    The calls run on the current stream, whichever it is; one at a time, since they share the scratch: calls on two streams
+    have to be ordered by events, and the object has to outlive those that are not on the stream that it was made on."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, length: torch.Tensor, *,
                  n_q_heads: int, pos: Optional[torch.Tensor] = None, score: Optional[torch.Tensor] = None):
@@ -473,6 +476,8 @@ class D2OPagedCache:
         _check(self.lib.d2o_paged_workspace_size(C.byref(self.cache), C.byref(n)), "d2o_paged_workspace_size")
         self.scratch = torch.empty(n.value + 256, dtype=torch.uint8, device=dev)
         self.scratch[:PAGED_ZERO_BYTES + 256].zero_()
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(dev).synchronize()                # cleared before a call on any other stream
         self._scratch = ((self.scratch.data_ptr() + 255) // 256 * 256, n.value)
         self._ref = C.byref(self.cache)
 
@@ -504,8 +509,10 @@ class D2OPagedCache:
               _arg(next_pos, "next_pos", (b,), torch.int32, x), n_sink, window, *self._scratch)
 
     def check(self):
-        """Raises if a call on this cache has met a bad length or page number since the last check.  Synchronises."""
+        """Raises if a call on this cache has met a bad length or page number since the last check.  Waits for all work on its GPU."""
+        torch.cuda.synchronize(self.device)
         word, detail = self.status.tolist()
         if word:
             self.status.zero_()
+            torch.cuda.synchronize(self.device)
             _check(word, f"paged cache (detail {detail & 0xffffffff:#x})")

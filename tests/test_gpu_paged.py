@@ -355,6 +355,27 @@ def test_streams_at_once(cuda_device):
         assert torch.equal(a[4], want[0]) and torch.equal(b[4], want[1]) and torch.equal(o, want[2])
 
 
+def test_made_on_one_stream_used_on_another(cuda_device):
+    """The scratch is cleared when the constructor returns, also behind work that is under way on its stream."""
+    a = _batch(3, 20, 8, 4, 128, "bf16", 16, 1500)
+    a[0].d2o_paged_decode_step(a[1], a[2], a[3], a[4])
+    want, size = a[4].clone(), a[0].scratch.numel()
+    k, v, table, length, _, _ = a[0].tensors
+    x = torch.randn(8192, 8192, device="cuda")
+    torch.full((size,), 255, dtype=torch.uint8, device="cuda")                 # what the next allocation of this size may find
+    torch.cuda.synchronize()
+    for _ in range(4):
+        x @ x
+    c = B.D2OPagedCache(k, v, table, length, n_q_heads=32)
+    assert torch.cuda.current_stream().query()
+    side, out = torch.cuda.Stream(), torch.zeros_like(want)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.d2o_paged_decode_step(a[1], a[2], a[3], out)
+    c.check()                                                                  # waits for the side stream too
+    assert torch.equal(out, want)
+
+
 def test_one_scratch_for_several_caches(cuda_device):
     """Caches of other shapes in turn on one scratch, as large as the largest asks for."""
     caches = [_batch(i, b, hkv, G, d, dt, 16, held, True) for i, (b, hkv, G, d, dt, held) in enumerate(
