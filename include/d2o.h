@@ -304,7 +304,7 @@ d2o_status d2o_layer_stats_static(int32_t dtype, int32_t d_head, int32_t batch, 
  * row's largest; sums and lse from the unrounded weights); fp32 inputs on CUDA cores, in fp32 throughout.
  * status DEVICE uint32 [2], may be NULL: error word and detail (D2O_ERR_TIMEOUT: a device-side wait ran out; rows that were in
  * hand are NaN).  No context, no scratch; asynchronous.
- * Limits: B * Hq * P < 2^31; d_head 64 or 128; Hq / Hkv any whole number. */
+ * Limits: P <= 2^20; B * Hq * P < 2^31; d_head 64 or 128; Hq / Hkv any whole number. */
 d2o_status d2o_prompt_attention(int32_t dtype, int32_t d_head, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
                                 int32_t prompt_len, int32_t window, int32_t n_sink, const void* Q, const void* K,
                                 const void* V, const int32_t* lens, void* out, float* lse, uint32_t* status, void* stream);
@@ -316,18 +316,19 @@ d2o_status d2o_prompt_attention(int32_t dtype, int32_t d_head, int32_t batch, in
  *
  * Rows of a sequence may lie in pages that another sequence's table names too (a common prefix) as long as nothing is written
  * there: the page that d2o_paged_decode_step or d2o_paged_append writes to, and with `score` every page of a sequence, belongs
- * to one sequence and stands in its table once.  Otherwise the rows and scores written there are undefined.
+ * to one sequence and stands in its table once.  Otherwise the contents of the pools and the outputs of the call are undefined,
+ * but nothing outside them is touched.
  *
  * What a call reads on the device is checked there: a page number outside 0 .. n_pages - 1, or a length that the table does
  * not reach, sets the error word and nothing is read or written through it (see each call). */
 typedef struct {
   int32_t dtype;                 /* d2o_dtype of pages, inputs and outputs                                           */
   int32_t d_head;                /* 64 or 128                                                                        */
-  int32_t batch;                 /* [B] sequences                                                                    */
+  int32_t batch;                 /* [B] sequences; batch * n_kv_heads <= 65535                                       */
   int32_t n_q_heads, n_kv_heads; /* n_q_heads / n_kv_heads = 1, 2, 4 or 8                                            */
   int32_t page_size;             /* rows per page and KV head: a power of two, 16 .. 1024                            */
   int32_t n_pages;               /* pages of the pools; n_pages * n_kv_heads * page_size < 2^31                      */
-  int32_t max_pages;             /* entries per row of page_table                                                    */
+  int32_t max_pages;             /* entries per row of page_table; max_pages * page_size < 2^30                      */
   void*    k_pages;              /* DEVICE [n_pages, Hkv, page_size, d]                                              */
   void*    v_pages;              /* DEVICE [n_pages, Hkv, page_size, d]                                              */
   int32_t* pos;                  /* DEVICE [n_pages, Hkv, page_size] original position of each row; NULL: not kept   */
@@ -347,7 +348,7 @@ typedef struct {
 d2o_status d2o_paged_workspace_size(const d2o_paged_cache* cache, size_t* bytes);
 
 /* Puts the rows of a prompt, or of a turn, behind those held: row i of sequence b goes to row len[b, h] + i, for i < lens[b].
- * K, V DEVICE [B, Hkv, n_rows, d]; lens DEVICE int32 [B] (0 .. n_rows; NULL: n_rows each).  With pos and score: row i gets
+ * K, V DEVICE [B, Hkv, n_rows, d], n_rows <= 2^30; lens DEVICE int32 [B] (0 .. n_rows; NULL: n_rows each).  With pos and score: row i gets
  * position first_pos[b] + i (DEVICE int32 [B]; NULL: i) and, as score, the sum of colsum [B, Hq, n_rows] over the query heads of
  * its KV head in their order (DEVICE float, the column sums of d2o_layer_stats: Eq. 6 case 1; NULL: 0).  first_pos and colsum
  * without pos and score are D2O_ERR_INVALID_ARG.  Rows that the table does not reach, or whose page number is bad, are not

@@ -654,6 +654,7 @@ extern "C" d2o_status d2o_paged_append(const d2o_paged_cache* cache, int32_t n_r
   const d2o_status st = validate_paged(cache, &p);
   if (st != D2O_OK) return st;
   if (n_rows < 1 || !aligned16(K) || !aligned16(V)) return D2O_ERR_INVALID_ARG;
+  if (n_rows > 1 << 30) return D2O_ERR_UNSUPPORTED;
   if ((first_pos || colsum) && !p.pos) return D2O_ERR_INVALID_ARG;
   if (((uintptr_t)lens | (uintptr_t)first_pos | (uintptr_t)colsum) & 3) return D2O_ERR_INVALID_ARG;
   CUDA_TRY(launch_paged_append(p, cache->dtype, cache->d_head, n_rows, K, V, lens, first_pos, colsum, (cudaStream_t)stream));

@@ -340,6 +340,8 @@ evict_kernel(EvictArgs a) {
   });
   sync_all();
   // ---- the moves
+  // Where two sequences' tables name the same page the numberings may disagree, and an entry may be old: nothing outside the pools.
+  const unsigned pool_rows = (unsigned)(p.n_pages * p.Hkv) << p.page_shift;
   const int grp = tid / LPR, lig = tid % LPR;
   int2 next[kEvictMoves];                                    // the following moves, read beside the rows of these
   auto look = [&](int k0) {
@@ -347,6 +349,7 @@ evict_kernel(EvictArgs a) {
     for (int u = 0; u < kEvictMoves; ++u) {
       const int k = k0 + u * C * GRPS;
       next[u] = k < moves ? a.moves[pool_row(k)] : make_int2(-1, -1);
+      if ((unsigned)next[u].x >= pool_rows || (unsigned)next[u].y >= pool_rows) next[u].x = -1;
     }
   };
   look(rank * GRPS + grp);

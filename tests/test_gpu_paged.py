@@ -464,6 +464,31 @@ def test_evict_long(cuda_device, n, budget, b, hkv):
 
 
 # ---------------------------------------------------------------------------------------------- anomalies
+@pytest.mark.parametrize("n", [1500, 30000])
+def test_evict_same_pages_in_two_tables(cuda_device, n):
+    """Against the documentation: what the pools hold afterwards is undefined, what lies around them stays, and later calls are right."""
+    page, d, hkv = 16, 64, 2
+    per = (n + page - 1) // page
+    g = torch.Generator(device="cuda").manual_seed(n)
+    guard = 4 * hkv * page * d
+    pools = [torch.full((2 * guard + (per + 1) * hkv * page * w,), 5, dtype=dt, device="cuda") for w, dt in ((d, torch.float16), (d, torch.float16), (1, torch.int32), (1, torch.float32))]
+    inner = [x[guard:-guard] for x in pools]
+    kp, vp = (x.view(per + 1, hkv, page, d) for x in inner[:2])
+    pos, score = (x.view(per + 1, hkv, page) for x in inner[2:])
+    pos.copy_(torch.randint(0, 1 << 20, pos.shape, generator=g, device="cuda"))
+    table = torch.randperm(per + 1, generator=g, device="cuda")[:per].to(torch.int32).expand(4, per).contiguous()
+    length = torch.full((4, hkv), n, dtype=torch.int32, device="cuda")
+    c = B.D2OPagedCache(kp, vp, table, length, n_q_heads=hkv, pos=pos, score=score)
+    c.scratch[B.PAGED_ZERO_BYTES + 256:].fill_(0x7F)                           # entries that no call wrote name rows far outside
+    budgets = torch.tensor([n // 5, n // 2, n // 3, n - 7], dtype=torch.int32, device="cuda")[:, None].expand(4, hkv).contiguous()
+    for _ in range(3):
+        c.d2o_paged_evict(budgets, torch.full((4,), 1 << 20, dtype=torch.int32, device="cuda"))
+    c.check()
+    for x in pools:
+        assert bool((x[:guard] == 5).all()) and bool((x[-guard:] == 5).all())
+    test_evict_long(cuda_device, 20000, 3000, 1, 8)
+
+
 def test_bad_tables(cuda_device):
     """Page numbers out of range and tables that are too short: reported, nothing read or written through them; other sequences go on."""
     def fresh():

@@ -52,6 +52,8 @@ def test_calls_refuse(lib):
         assert append(cache(**kw), 1, 256, 256, None, None, None) == status, kw
         assert step(cache(**kw), 0, 0, 256, 256, 256, None, 256, 256, n) == status, kw
         assert evict(cache(**kw), 256, 256, 0, 0, 256, n) == status, kw
+    for n_rows in ((1 << 30) + 1, (1 << 31) - 1):
+        assert append(cache(), n_rows, 256, 256, None, None, None) == 2
     bare = cache(pos=None, score=None)
     for a in [(0, 256, 256, None, None, None), (1, None, 256, None, None, None), (1, 256, 264, None, None, None), (1, 256, 256, 2, None, None)]:
         assert append(cache(), *a) == 1, a
