@@ -607,6 +607,9 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     for (int i = 0; i < BUFS; ++i) { tc::mbar_init(&s_written[i], WARPS); tc::mbar_init(&s_free[i], 1); }
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  // A warp without a tile arrives at the shared mbarriers after one load: their initialisation comes first.  (The shares have a barrier of the
+  // CTA in paged_start.)
+  if (CL) __syncthreads();
   wait_for_prior_grid();
   __syncwarp();
   asm volatile("fence.proxy.async.global;" ::: "memory");    // rows that kernels ahead wrote with ordinary stores are read by copies

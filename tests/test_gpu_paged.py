@@ -325,6 +325,23 @@ def test_decode_many(cuda_device, b, hkv, G, d, dtype, held):
     assert not c.scratch[zero:zero + B.PAGED_ZERO_BYTES].any()                 # as every call leaves them
 
 
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("f16", 64, 1), ("bf16", 64, 8), ("f16", 128, 2)])
+def test_decode_clusters_of_idle_warps(cuda_device, dtype, d, G):
+    """Slices with a cluster each and a tile or two in all, so that most warps, and whole CTAs, have nothing to do and are at the shared barriers
+    first: many launches in a row, nothing lost, the same bits."""
+    c, q, k, v, out, check = _batch(d + G, 2, 4, G, d, dtype, 16, 40)
+    check_all = [(i, h) for i in range(2) for h in range(4)]
+    for n in (0, 1, 15, 16, 40):
+        c.tensors[3].fill_(n)
+        c.d2o_paged_decode_step(q, k, v, out)
+        check(out, check_all)
+        outs = torch.zeros(200, *q.shape, dtype=q.dtype, device="cuda")
+        for x in outs:
+            c.d2o_paged_decode_step(q, k, v, x)
+        c.check()
+        assert bool((outs == out).all())
+
+
 def test_streams_at_once(cuda_device):
     """Steps on two caches, an eviction on a third and a prompt's attention, on four streams at the same time, many times over: the bits
     of the same calls one after another."""
