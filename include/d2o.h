@@ -302,8 +302,8 @@ d2o_status d2o_layer_stats_static(int32_t dtype, int32_t d_head, int32_t batch, 
  * not (0 * inf).
  * 16-bit inputs run on the tensor cores, the weights p rounded to the input type for their product with V (relative to the
  * row's largest; sums and lse from the unrounded weights); fp32 inputs on CUDA cores, in fp32 throughout.
- * status DEVICE uint32 [2], may be NULL: error word and detail (D2O_ERR_TIMEOUT: a device-side wait ran out; rows that were in
- * hand are NaN).  No context, no scratch; asynchronous.
+ * status DEVICE uint32 [2], may be NULL: error word and detail (D2O_ERR_TIMEOUT: a device-side wait ran out; the rows of every thread
+ * block that it happened in, and of the work that it had taken over, are NaN).  No context, no scratch; asynchronous.
  * Limits: P <= 2^20; B * Hq * P < 2^31; d_head 64 or 128; Hq / Hkv any whole number. */
 d2o_status d2o_prompt_attention(int32_t dtype, int32_t d_head, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
                                 int32_t prompt_len, int32_t window, int32_t n_sink, const void* Q, const void* K,
@@ -409,6 +409,12 @@ d2o_status d2o_set_tuning(d2o_ctx* ctx, int32_t decode_stages, int32_t decode_l2
  * whose wait ran out during the key pass are left untouched, the call's other slices may or may not have taken the step, and
  * every later decode step on this context does nothing.  Nothing traps and the CUDA context stays usable. */
 d2o_status d2o_set_fault_injection(d2o_ctx* ctx, int32_t wait_limit_us, int32_t producer_stop_stage);
+
+/* The same for d2o_prompt_attention (16-bit inputs), which has no context: for the whole process, from the next
+ * call on (a call captured into a graph keeps what held when it was captured).  producer_stop_stage: no tile of keys or values
+ * is copied from this one of every thread block on (-1 = never).  late_answers = 1: the answers by which thread blocks take over
+ * the work of others count as late.  (0, -1, 0) is the ordinary state. */
+d2o_status d2o_set_static_fault_injection(int32_t wait_limit_us, int32_t producer_stop_stage, int32_t late_answers);
 
 #ifdef __cplusplus
 }

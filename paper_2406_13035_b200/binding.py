@@ -25,7 +25,7 @@ EXPORTS = [
     "d2o_status_string", "d2o_last_cuda_error", "d2o_workspace_size", "d2o_create", "d2o_destroy",
     "d2o_layer_stats", "d2o_layer_stats_layers", "d2o_layer_budgets", "d2o_budgets_from_density", "d2o_prefill_compress",
     "d2o_prefill_compress_layers", "d2o_decode_step", "d2o_decode_steps", "d2o_decode_step_host", "d2o_decode_steps_host", "d2o_full_decode_step", "d2o_get_view", "d2o_get_stats",
-    "d2o_set_tuning", "d2o_layer_stats_static", "d2o_set_fault_injection", "d2o_set_prompt_lens",
+    "d2o_set_tuning", "d2o_layer_stats_static", "d2o_set_fault_injection", "d2o_set_static_fault_injection", "d2o_set_prompt_lens",
     "d2o_prompt_attention", "d2o_paged_workspace_size", "d2o_paged_append", "d2o_paged_decode_step", "d2o_paged_evict",
 ]
 STATIC_LSE_FLOATS = 1 << 20      # D2O_STATIC_LSE_FLOATS of include/d2o.h
@@ -114,6 +114,7 @@ def load_library() -> C.CDLL:
     lib.d2o_set_tuning.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32]
     lib.d2o_layer_stats_static.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
     lib.d2o_set_fault_injection.argtypes = [vp, i32, i32]
+    lib.d2o_set_static_fault_injection.argtypes = [i32, i32, i32]
     lib.d2o_set_prompt_lens.argtypes = [vp, vp, vp]
     pg = C.POINTER(D2OPaged)
     lib.d2o_prompt_attention.argtypes = [i32] * 8 + [vp] * 8
@@ -441,6 +442,11 @@ def d2o_prompt_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out:
           _arg(V, "V", (b, hkv, n, d), Q.dtype, dev), _arg(lens, "lens", (b,), torch.int32, dev),
           _arg(out, "out", (b, hq, n, d), Q.dtype, dev), _arg(lse, "lse", (b, hq, n), torch.float32, dev),
           _arg(status, "status", (2,), torch.int32, dev))
+
+
+def d2o_set_static_fault_injection(wait_limit_us: int = 0, producer_stop_stage: int = -1, late_answers: bool = False):
+    """For failure-detection tests of the calls without a context; the defaults are the ordinary state."""
+    _check(load_library().d2o_set_static_fault_injection(wait_limit_us, producer_stop_stage, int(late_answers)), "d2o_set_static_fault_injection")
 
 
 class D2OPagedCache:

@@ -97,7 +97,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   unsigned char* sKV = pa_smem + 2 * TILE;                   // [stages][KB][128 rows][128 B]
   __shared__ unsigned long long q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2][2], o_full[2], o_empty[2], turn[2], all_done[2], it_full[2], it_empty[2], answered;
   __shared__ alignas(16) uint4 s_answer;
-  __shared__ volatile int s_item[2], s_lost;                 // this CTA's current and next item; taken after a wait had run out; -1: none
+  __shared__ volatile int s_item[2], s_lost;                 // this CTA's current and next item; given to it after a wait had run out; -1: none
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_fail;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -121,13 +121,13 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   const uint32_t tm_s = s_tmem, tm_o = s_tmem + 256;         // S (and P) of tile t at + 128 t, O at + 128 t
   auto wait = [&](unsigned long long* bar, uint32_t parity) {
     if (tc::mbar_try_wait(bar, parity)) return true;
-    if (!s_fail && tc::mbar_wait(bar, parity)) return true;
+    if (!s_fail && tc::mbar_wait(bar, parity, a.wait_ns)) return true;
     s_fail = 1;
     return false;
   };
   start_dependents();
   wait_for_prior_grid();
-  int loads_q = 0, loads_kv = 0;                             // of the producer
+  int loads_q = 0, loads_kv = 0, unanswered = -1;            // of the producer; the request whose answer was not there in time
   // The k-th item of this CTA as a warp sees it; -1: no more.
   auto next_item = [&](int k) {
     if (!__all_sync(0xffffffffu, wait(&it_full[k & 1], (uint32_t)((k >> 1) & 1)))) return -1;
@@ -155,6 +155,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         const int q_row = it.bh * a.P + it.q0, k_base = (it.b * a.Hkv + it.bh % a.Hq / (a.Hq / a.Hkv)) * a.P;
         for (int j = 0; j < (it.empty() ? 0 : 2 * span.tiles); ++j) {      // K, V, K, V ..
           const int s = loads_kv % STAGES;
+          if (loads_kv == a.stop_stage) goto stopped;
           if (loads_kv >= STAGES && !wait(&kv_empty[s], (uint32_t)((loads_kv / STAGES - 1) & 1))) break;
           tc::mbar_expect_tx(&kv_full[s], TILE);
           for (int kb = 0; kb < KB; ++kb)
@@ -171,8 +172,13 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         // Not earlier: the loads are two tiles of keys ahead of the products, which covers the answer's way, and an item asked for at the
         // beginning of a long one would wait while other CTAs have nothing to do (1200 tokens of 32 heads: 36 us instead of 30).
         tc::ask_for_cta(&s_answer, &answered);
-        i = tc::mbar_wait(&answered, (uint32_t)(k & 1)) ? tc::cta_answered(&s_answer) : -1;
+        if (!a.late_answers && wait(&answered, (uint32_t)(k & 1))) {
+          i = tc::cta_answered(&s_answer);
+        } else {                                             // the CTA that it may name will not start: looked at again below
+          s_fail = 1; unanswered = k; i = -1;
+        }
       }
+      stopped:;
     }
     __syncwarp();
   } else if (warp < kPaSoftWarps + 3) {
@@ -362,8 +368,10 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       for (int i = max(0, loads_kv - STAGES); i < loads_kv; ++i)
         if (!tc::mbar_wait(&kv_full[i % STAGES], (uint32_t)((i / STAGES) & 1))) break;
       if (loads_q > 0) (void)tc::mbar_wait(&q_full, (uint32_t)((loads_q - 1) & 1));
+      if (unanswered >= 0 && tc::mbar_wait(&answered, (uint32_t)(unanswered & 1))) s_lost = tc::cta_answered(&s_answer);
       if (a.status) report_error(a.status, D2O_ERR_TIMEOUT, 0xA7710000u | (uint32_t)(blockIdx.x & 0xffff));
     }
+    __syncthreads();
     for (int x = 0; x < 3; ++x) {                            // NaN for the items in hand
       const int i = x < 2 ? s_item[x] : s_lost;
       if (i < 0) continue;

@@ -14,6 +14,7 @@ namespace d2o {
 
 constexpr float kEuler = 2.718281828459045f;   // weight of a conserved token: exp(self-similarity 1), Eq. 12
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr unsigned long long kDeviceWaitNs = 1000000000ull;   // limit of a wait on the device, unless a test sets another
 
 // ----------------------------------------------------------------------------- element traits
 template <typename T> struct Elem;

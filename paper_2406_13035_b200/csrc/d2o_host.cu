@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "d2o_attention.cuh"
 #include "d2o_common.cuh"
@@ -584,6 +585,22 @@ extern "C" d2o_status d2o_full_decode_step(int32_t dtype, int32_t d_head, int32_
 }
 
 // ------------------------------------------------------------------------------------ prompt attention, cache in pages
+// d2o_set_static_fault_injection: of the whole process, read by every call that follows
+static std::atomic<int> g_wait_limit_us{0}, g_stop_stage{-1}, g_late_answers{0};
+
+extern "C" d2o_status d2o_set_static_fault_injection(int32_t wait_limit_us, int32_t producer_stop_stage, int32_t late_answers) {
+  if (wait_limit_us < 0 || producer_stop_stage < -1 || late_answers < 0 || late_answers > 1) return D2O_ERR_INVALID_ARG;
+  g_wait_limit_us = wait_limit_us;
+  g_stop_stage = producer_stop_stage;
+  g_late_answers = late_answers;
+  return D2O_OK;
+}
+
+static unsigned long long static_wait_ns() {
+  const int us = g_wait_limit_us;
+  return us > 0 ? (unsigned long long)us * 1000ull : kDeviceWaitNs;
+}
+
 extern "C" d2o_status d2o_prompt_attention(int32_t dtype, int32_t d_head, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads,
                                            int32_t prompt_len, int32_t window, int32_t n_sink, const void* Q, const void* K,
                                            const void* V, const int32_t* lens, void* out, float* lse, uint32_t* status,
@@ -600,6 +617,7 @@ extern "C" d2o_status d2o_prompt_attention(int32_t dtype, int32_t d_head, int32_
   a.B = batch; a.Hq = n_q_heads; a.Hkv = n_kv_heads; a.P = prompt_len;
   a.window = window > 0 ? std::min(window, prompt_len) : prompt_len;
   a.n_sink = std::min(n_sink, prompt_len);
+  a.wait_ns = static_wait_ns(); a.stop_stage = g_stop_stage; a.late_answers = g_late_answers;
   CUDA_TRY(launch_prompt_attention(dtype, d_head, a, (cudaStream_t)stream));
   return D2O_OK;
 }

@@ -8,7 +8,7 @@
 
 namespace d2o {
 
-constexpr unsigned long long kTcWaitNs = 1000000000ull;   // an mbarrier wait gives up after 1 s
+constexpr unsigned long long kTcWaitNs = kDeviceWaitNs;   // an mbarrier wait gives up after 1 s
 
 // ----------------------------------------------------------------------------- PTX wrappers
 namespace tc {
@@ -37,7 +37,7 @@ __device__ __forceinline__ bool mbar_wait(unsigned long long* bar, uint32_t pari
   if (mbar_try_wait(bar, parity)) return true;
   const unsigned long long t0 = global_ns();
   while (!mbar_try_wait(bar, parity)) {
-    if (global_ns() - t0 > limit_ns) return false;
+    if (global_ns() - t0 > limit_ns) return mbar_try_wait(bar, parity);      // once more: the limit may have passed while this warp did not run
   }
   return true;
 }
