@@ -362,7 +362,9 @@ d2o_status d2o_paged_append(const d2o_paged_cache* cache, int32_t n_rows, const 
  * q, out DEVICE [B, Hq, d]; k, v DEVICE [B, Hkv, d].  With pos and score: row t gets positions[b] (DEVICE int32 [B]; NULL: t),
  * its weight, summed over the query heads, as score, and every other row that is seen has its weight added to its score (Eq. 6
  * case 2).  A sequence whose table does not reach row t gets NaN outputs, and one that
- * has a bad page number among the rows seen NaN outputs and scores, in the heads concerned; both set the error word.  Rows outside the view may hold anything.  The caller adds one to len.
+ * has a bad page number among the rows seen NaN outputs and scores, in the heads concerned; both set the error word.  So does a
+ * device-side wait that runs out (D2O_ERR_TIMEOUT), with NaN outputs and scores in the heads concerned, whose new row may not have been
+ * written.  Rows outside the view may hold anything.  The caller adds one to len.
  * The rows of all sequences together are divided evenly over the GPU, whatever the single lengths, and what was divided is
  * joined again in a fixed order: results do not change from run to run.  Asynchronous. */
 d2o_status d2o_paged_decode_step(const d2o_paged_cache* cache, int32_t window, int32_t n_sink, const void* q, const void* k,
@@ -410,10 +412,11 @@ d2o_status d2o_set_tuning(d2o_ctx* ctx, int32_t decode_stages, int32_t decode_l2
  * every later decode step on this context does nothing.  Nothing traps and the CUDA context stays usable. */
 d2o_status d2o_set_fault_injection(d2o_ctx* ctx, int32_t wait_limit_us, int32_t producer_stop_stage);
 
-/* The same for d2o_prompt_attention (16-bit inputs), which has no context: for the whole process, from the next
- * call on (a call captured into a graph keeps what held when it was captured).  producer_stop_stage: no tile of keys or values
- * is copied from this one of every thread block on (-1 = never).  late_answers = 1: the answers by which thread blocks take over
- * the work of others count as late.  (0, -1, 0) is the ordinary state. */
+/* The same for the 16-bit kernels of d2o_prompt_attention and d2o_paged_decode_step, which have no context: for the whole process, from the next
+ * call on (a call captured into a graph keeps what held when it was captured).  producer_stop_stage: the prompt attention copies no tile of
+ * keys or values from this one of every thread block on, the decode step does not copy the tile of this number (-1 = never).
+ * late_answers = 1: the answers by which thread blocks of the prompt attention take over the work of others count as late.  (0, -1, 0) is
+ * the ordinary state. */
 d2o_status d2o_set_static_fault_injection(int32_t wait_limit_us, int32_t producer_stop_stage, int32_t late_answers);
 
 #ifdef __cplusplus

@@ -690,7 +690,7 @@ extern "C" d2o_status d2o_paged_decode_step(const d2o_paged_cache* cache, int32_
   st = validate_scratch(cache, scratch, scratch_bytes);
   if (st != D2O_OK) return st;
   CUDA_TRY(launch_paged_decode(p, cache->dtype, cache->d_head, window, n_sink, q, k, v, positions, out, (char*)scratch,
-                               (cudaStream_t)stream));
+                               (cudaStream_t)stream, static_wait_ns(), g_stop_stage));
   return D2O_OK;
 }
 

@@ -52,7 +52,8 @@ struct PagedSpan {
 cudaError_t launch_paged_append(const PagedView& p, int dtype, int D, int n_rows, const void* K, const void* V, const int32_t* lens,
                                 const int32_t* first_pos, const float* colsum, cudaStream_t st);
 cudaError_t launch_paged_decode(const PagedView& p, int dtype, int D, int window, int n_sink, const void* q, const void* k,
-                                const void* v, const int32_t* positions, void* out, char* scratch, cudaStream_t st);
+                                const void* v, const int32_t* positions, void* out, char* scratch, cudaStream_t st, unsigned long long wait_ns,
+                                int stop_stage);
 cudaError_t launch_paged_evict(const PagedView& p, int dtype, int D, const int32_t* budgets, const int32_t* next_pos, int n_sink,
                                int window, char* scratch, cudaStream_t st);
 

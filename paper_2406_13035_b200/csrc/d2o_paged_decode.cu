@@ -47,6 +47,8 @@ struct PagedDecodeArgs {
   float* lse2;                               // [slices][G] normalisers in the log2 domain (with scores)
   float* parts;                              // [ctas][2][G][D + 4]: output, maximum, sum, -; 0: of a slice that ends in the share, 1: that goes on
   float* logits;                             // per row of the pools, G logits in the log2 domain (with scores)
+  unsigned long long wait_ns;                // limit of every wait (16-bit kernel)
+  int stop_stage;                            // failure-detection tests: the tile of this number of every CTA's share is not copied; -1: none
 };
 
 // a / b; nearly always both fit 32 bits, and a division of 64 bits is a hundred instructions
@@ -532,9 +534,9 @@ struct PagedCursor {
 __host__ __device__ constexpr int paged_buffers(int G) { return G <= 2 ? 2 : 1; }
 
 // One warp adds the results of all warps for one part ([warps][G][LD] outputs, [warps][G, even] maxima and sums): the slice's output, or a part
-// for the joins in `to` ([G][D + 4]).
+// for the joins in `to` ([G][D + 4]).  `lost`: not all results are there, NaN.
 template <typename T, int D, int G, int LD>
-__device__ __forceinline__ void combine_warps(const PagedDecodeArgs& a, int sl, int b, int h, bool whole, float* to, const float* red, const float* s_m, const float* s_l) {
+__device__ __forceinline__ void combine_warps(const PagedDecodeArgs& a, int sl, int b, int h, bool whole, bool lost, float* to, const float* red, const float* s_m, const float* s_l) {
   constexpr int WARPS = paged_warps(G);
   static_assert(WARPS <= 16, "sixteen lanes per head");
   constexpr int LPR = D / 4, HEADS = 32 / LPR, N = (G + 1) / 2;          // lanes per row of D floats, heads at a time; factors per lane
@@ -550,7 +552,7 @@ __device__ __forceinline__ void combine_warps(const PagedDecodeArgs& a, int sl, 
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) mc = fmaxf(mc, __shfl_xor_sync(0xffffffffu, mc, o));
     f[e] = m > -INFINITY ? exp2f(m - mc) : mc > -INFINITY ? 0.f : 1.f;
-    l = l != l ? NAN : l * f[e];                             // a NaN sum of a bad page stays
+    l = lost || l != l ? NAN : l * f[e];                     // a NaN sum of a bad page stays
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     lc[e] = l;
@@ -635,7 +637,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     if (lane == 0) {
       s_row[warp][s] = row;
       unsigned char* to = my_ring + s * 2 * TILE;
-      if (row >= 0) {
+      if (a.stop_stage >= 0 && at - first == a.stop_stage) {             // never arrives
+      } else if (row >= 0) {
         tc::mbar_expect_tx(&s_full[warp][s], 2 * TILE);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
@@ -675,10 +678,9 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   long long mine = first + warp;                             // this warp's next tile
   int taken = 0, parts = 0;
   PagedOpen open;
-  bool lost = false;                                         // a wait ran out: NaN from here on
-  auto land = [&]() {                                        // sees the copies on their way land before the CTA may end
-    for (int i = max(0, asked - STAGES); i < asked; ++i)
-      if (!tc::mbar_wait(&s_full[warp][i % STAGES], (uint32_t)((i / STAGES) & 1))) break;
+  bool lost = false;                                         // a wait of this warp ran out: NaN from here on
+  auto wait = [&](unsigned long long* bar, uint32_t phase) {             // of the whole warp
+    lost = __any_sync(0xffffffffu, lost || !tc::mbar_wait(bar, phase, a.wait_ns));
   };
   while (cur.at < last) {
     const PagedSpan& span = cur.span;
@@ -697,10 +699,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     for (int i = 0; i < D / 16; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
     for (; mine < end; mine += WARPS) {
       const int s = taken % STAGES;
-      if (!lost && !tc::mbar_wait(&s_full[warp][s], (uint32_t)((taken / STAGES) & 1))) {
-        lost = true;
-      }
-      lost = __any_sync(0xffffffffu, lost);
+      if (!lost) wait(&s_full[warp][s], (uint32_t)((taken / STAGES) & 1));
       ++taken;
       const int row0 = span.row0((int)(mine - cur.before)), prow = s_row[warp][s];
       unsigned char* stage = my_ring + s * 2 * TILE;
@@ -786,12 +785,14 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     for (int o = 4; o < 32; o <<= 1) { l[0] += __shfl_xor_sync(0xffffffffu, l[0], o); l[1] += __shfl_xor_sync(0xffffffffu, l[1], o); }
     const int buf = parts % BUFS;
     const uint32_t phase = (uint32_t)((parts / BUFS) & 1);
-    if (parts >= BUFS && !lost && !tc::mbar_wait(&s_free[buf], phase ^ 1)) lost = true;
+    if (parts >= BUFS && !lost) wait(&s_free[buf], phase ^ 1);
     float* mine_red = red + (size_t)buf * WARPS * G * LD + warp * G * LD;
     if (gid == 0 && 2 * tig < G) {
-      s_m[buf][warp][2 * tig] = m[0]; s_m[buf][warp][2 * tig + 1] = m[1];
-      s_l[buf][warp][2 * tig] = l[0]; s_l[buf][warp][2 * tig + 1] = l[1];
+      // without the buffer, which may be read for the part before: a NaN sum alone, which makes either part NaN
+      if (!lost) { s_m[buf][warp][2 * tig] = m[0]; s_m[buf][warp][2 * tig + 1] = m[1]; }
+      s_l[buf][warp][2 * tig] = lost ? NAN : l[0]; s_l[buf][warp][2 * tig + 1] = lost ? NAN : l[1];
     }
+    if (!lost)
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       float* to = mine_red + 2 * tig * LD + i * 16 + gid;
@@ -803,10 +804,9 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     const int i0 = (int)(cur.at - cur.before), i1 = (int)(end - cur.before);
     const bool whole = !CL && i0 == 0 && i1 == span.tiles;
     if (warp == parts % WARPS) {
-      if (!lost && !tc::mbar_wait(&s_written[buf], phase)) lost = true;
-      if (CL && lost) land();                                // the part goes to the ring's place
+      if (!lost) wait(&s_written[buf], phase);
       float* to = CL ? reinterpret_cast<float*>(paged_smem) : a.parts + ((size_t)c * 2 + (end < cur.before + span.tiles ? 1 : 0)) * G * (D + 4);
-      combine_warps<T, D, G, LD>(a, sl, b, h, whole, to, red + (size_t)buf * WARPS * G * LD, &s_m[buf][0][0], &s_l[buf][0][0]);
+      combine_warps<T, D, G, LD>(a, sl, b, h, whole, lost, to, red + (size_t)buf * WARPS * G * LD, &s_m[buf][0][0], &s_l[buf][0][0]);
       __syncwarp();
       if (lane == 0) tc::mbar_arrive(&s_free[buf]);
     }
@@ -815,12 +815,15 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     cur.at = end;
     cur.settle(a, last);
   }
-  lost = __any_sync(0xffffffffu, lost);
-  if (lost && lane == 0 && p.status) report_error(p.status, D2O_ERR_TIMEOUT, 0x9A6E3000u);
-  __syncthreads();                                           // the last parts are combined
+  if (__syncthreads_or(lost)) {                              // the last parts are combined
+    if (tid == 0 && p.status) report_error(p.status, D2O_ERR_TIMEOUT, 0x9A6E3000u);
+    // see the copies on their way land before the CTA may end, and before a cluster's part, which lies in the ring's place, is read
+    for (int i = max(0, asked - STAGES); i < asked; ++i) (void)tc::mbar_wait(&s_full[warp][i % STAGES], (uint32_t)((i / STAGES) & 1), a.wait_ns);
+    __syncthreads();
+    if (CL && tid < G) reinterpret_cast<float*>(paged_smem)[tid * (D + 4) + D + 1] = NAN;
+  }
   if (CL) join_cluster<T, D, G, WARPS>(a, start.slice, reinterpret_cast<float*>(paged_smem), first == last);
   else close_parts<T, D, G, WARPS>(a, start, open, red, s_join);
-  if (lost) land();
 }
 
 // Adds the weights to the scores of a slice's rows (blockIdx.x), divided over blockIdx.y.
@@ -923,7 +926,8 @@ static cudaError_t launch_g(const PagedDecodeArgs& a, cudaStream_t st) {
 }
 
 cudaError_t launch_paged_decode(const PagedView& p, int dtype, int D, int window, int n_sink, const void* q, const void* k,
-                                const void* v, const int32_t* positions, void* out, char* scratch, cudaStream_t st) {
+                                const void* v, const int32_t* positions, void* out, char* scratch, cudaStream_t st, unsigned long long wait_ns,
+                                int stop_stage) {
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return cudaGetLastError();
@@ -932,6 +936,7 @@ cudaError_t launch_paged_decode(const PagedView& p, int dtype, int D, int window
   PagedDecodeArgs a;
   a.p = p;
   a.q = q; a.k = k; a.v = v; a.out = out; a.positions = positions; a.window = window; a.n_sink = n_sink;
+  a.wait_ns = wait_ns; a.stop_stage = stop_stage;
   a.ctas = std::min(sms, kPagedCtas);
   a.done = reinterpret_cast<uint32_t*>(scratch + s.done);
   a.lse2 = reinterpret_cast<float*>(scratch + s.lse2);

@@ -72,3 +72,54 @@ def test_prompt_attention_whose_tiles_do_not_arrive(cuda_device, knob, dtype, d,
     knob()
     B.d2o_prompt_attention(q, k, v, out)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("f16", 64, 1), ("bf16", 64, 8), ("f16", 128, 2)])
+@pytest.mark.parametrize("b,hkv,held,room", [(1, 4, 900, 1000), (2, 8, 300, 2000), (3, 8, 2500, 20000), (60, 8, 200, 400), (400, 2, 70, 100), (1, 1, 9000, 60000)])
+@pytest.mark.parametrize("stage", [0, 1, 5, 13, 40])
+def test_decode_step_whose_tiles_do_not_arrive(cuda_device, knob, dtype, d, G, b, hkv, held, room, stage):
+    """One tile of every share is missing, in clusters and in shares of one or several slices: a slice's outputs are all NaN or right, never something
+    else, and its scores are NaN where its outputs are.  The step after it is right, and the counters in the scratch are zero again."""
+    page = 16
+    g = torch.Generator(device="cuda").manual_seed(held + d)
+    per, used = room // page, held // page + 1
+    n_pages = b * used + 1
+    table = torch.full((b, per), -1, dtype=torch.int32, device="cuda")
+    table[:, :used] = torch.randperm(n_pages, generator=g, device="cuda")[: b * used].view(b, used).to(torch.int32)
+    kp, vp = (torch.randn(n_pages, hkv, page, d, generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    length = torch.randint(0, held + 1, (b, hkv), generator=g, device="cuda", dtype=torch.int32)
+    length[0] = held
+    q, k, v = (torch.randn(b, h, d, generator=g, device="cuda").to(DT[dtype]) for h in (hkv * G, hkv, hkv))
+    pos, score = torch.zeros(n_pages, hkv, page, dtype=torch.int32, device="cuda"), torch.zeros(n_pages, hkv, page, device="cuda")
+    c = B.D2OPagedCache(kp, vp, table, length, n_q_heads=hkv * G, pos=pos, score=score)
+    want, out = torch.empty_like(q), torch.full_like(q, 7.0)
+    c.d2o_paged_decode_step(q, k, v, want)
+    want_score = score.clone()
+    c.check()
+    score.zero_()
+    knob(2000, stage)
+    _timed(lambda: c.d2o_paged_decode_step(q, k, v, out))
+    slices = lambda t: t.view(b, hkv, G * d)
+    bad = slices(out).isnan()
+    assert bool((bad.all(-1) == bad.any(-1)).all())
+    bad = bad.all(-1)
+    assert bool((bad | (slices(out) == slices(want)).all(-1)).all())
+    dense = lambda t: t[table[:, :used].long()].transpose(1, 2).flatten(2)
+    seen = torch.arange(used * page, device="cuda") <= length[..., None]
+    got, was = dense(score), dense(want_score)
+    assert bool((got.isnan() | ~seen)[bad].all()) and bool((got == was)[~bad].all()) and bool((got == 0)[~seen].all())
+    if stage == 0:
+        assert bool(bad.any())
+    if bool(bad.any()):
+        with pytest.raises(B.D2OError) as e:
+            c.check()
+        assert e.value.status == D2O_ERR_TIMEOUT
+    else:
+        c.check()
+    knob()
+    score.zero_()
+    c.d2o_paged_decode_step(q, k, v, out)
+    assert torch.equal(out, want) and torch.equal(score, want_score)
+    c.check()
+    zero = c._scratch[0] - c.scratch.data_ptr()
+    assert not c.scratch[zero:zero + B.PAGED_ZERO_BYTES].any()
