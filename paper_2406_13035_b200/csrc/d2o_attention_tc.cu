@@ -26,6 +26,7 @@
 
 #include "d2o_attention.cuh"
 #include "d2o_common.cuh"
+#include "d2o_decode.cuh"
 #include "d2o_tc.cuh"
 
 namespace d2o {
@@ -34,6 +35,7 @@ constexpr int kPaTile = 128;
 constexpr int kPaSoftWarps = 8;
 constexpr int kPaThreads = (kPaSoftWarps + 4) * 32;          // three warpgroups: registers move between whole ones
 constexpr float kPaSlack = 8.f;              // growth of the maximum (log2 domain) that the reference leaves standing
+constexpr float kPaFar = 1048576.f;          // references (log2 domain) beyond which their rounding is more than 1/16
 
 __host__ __device__ constexpr int pa_stages(int D) { return D == 128 ? 4 : 8; }
 
@@ -81,6 +83,73 @@ __device__ __forceinline__ void pa_block(const uint32_t (&s)[32], uint32_t (&p)[
     sum[i & 1] = tc::add2(sum[i & 1], tc::pack2(y0, y1));
     if (FMT == 0) { const __half2 h = __floats2half2_rn(y0, y1); p[AT + i] = *reinterpret_cast<const uint32_t*>(&h); }
     else { const __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1); p[AT + i] = *reinterpret_cast<const uint32_t*>(&h); }
+  }
+}
+
+// The rows r0 + (bits of `rows`) once more, by one warp, in fp32.  The weights 2^(c s - m) of the tensor-core path have the product c s unrounded
+// and m rounded: with logits in the millions their difference would be anything, from 0 to infinity.  Here c s is rounded before m is taken
+// from it.  For inputs that no trained model has: 8192 keys take 13 ms per 256 rows (ordinary ones 0.14), and with more than half a million the other
+// warps' waits run out.  A function, and behind the item, because any code for such rows in the loop over the tiles costs every prompt 2 - 8 %; this
+// one 0.5 %.
+template <typename T, int D>
+__device__ __noinline__ void pa_far_rows(const T* Q, const T* K, const T* V, T* out, float* lse, unsigned rows, int r0, int window, int n_sink) {
+  constexpr int LPR = D / 8, RPW = 32 / LPR, U = 8, QL = LPR / 4;        // lanes per row of 8 elements each, rows of a warp, in flight
+  const float c = (D == 64 ? 0.125f : 0.08838834764831845f) * kLog2e;
+  const int lane = threadIdx.x & 31, grp = lane / LPR, lig = lane % LPR;
+  for (; rows; rows &= rows - 1) {
+    const int r = r0 + __ffs(rows) - 1, lo = max(0, r - window + 1), sinks = min(n_sink, lo), n = sinks + r + 1 - lo;
+    auto at = [&](int i) { return (size_t)(i < sinks ? i : lo + i - sinks) * D + lig * 8; };       // of the i-th key that the row sees
+    float q[8], m = -INFINITY, l = 0.f, acc[8];
+    Elem<T>::unpack(ld_global_v4(Q + (size_t)r * D + lig * 8), q);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    for (int i0 = 0; i0 < n; i0 += U * RPW) {
+      uint4 kv[U], vv[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * RPW + grp;
+        kv[u] = vv[u] = make_uint4(0, 0, 0, 0);
+        if (i < n) { kv[u] = ld_global_v4(K + at(i)); vv[u] = ld_global_v4(V + at(i)); }
+      }
+      float x[U / 4], mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < U / 4; ++j) {
+        float dot[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          float k[8];
+          Elem<T>::unpack(kv[j * 4 + u], k);
+          dot[u] = dot_pairs<8>(q, k);
+        }
+        const float t = reduce4<LPR>(dot[0], dot[1], dot[2], dot[3], lig) * c;
+        x[j] = i0 + (j * 4 + lig / QL) * RPW + grp < n ? t : -INFINITY;
+        mx = fmaxf(mx, x[j]);
+      }
+      const float mn = fmaxf(m, warp_max(mx)), base = mn > -INFINITY ? mn : 0.f, f = exp2f(m - base);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] *= f;
+#pragma unroll
+      for (int j = 0; j < U / 4; ++j) { x[j] = exp2f(x[j] - base); l += x[j]; }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float w = __shfl_sync(0xffffffffu, x[u / 4], (u & 3) * QL, LPR);
+        float v[8];
+        Elem<T>::unpack(vv[u], v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = fmaf(w, v[e], acc[e]);
+      }
+    }
+    l = warp_sum(l) * (1.f / QL);                            // QL lanes had the same keys
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+#pragma unroll
+      for (int o = LPR; o < 32; o <<= 1) acc[e] += __shfl_xor_sync(0xffffffffu, acc[e], o);
+      acc[e] /= l;
+    }
+    if (lane < LPR) *reinterpret_cast<uint4*>(out + (size_t)r * D + lig * 8) = Elem<T>::pack(acc);
+    if (lse && lane == 0) lse[r] = (m + log2f(l)) * 0.6931471805599453f;
   }
 }
 
@@ -267,7 +336,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       if (it.empty() || !it.exists(t)) continue;
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
       const int w0 = it.q0 + t * kPaTile, r0 = w0 + quarter * 32, row = r0 + lane;      // first query of tile and warp, this thread's
-      float m = -INFINITY, l = 0.f;                          // reference (log2 domain), sum
+      float m = -INFINITY, l = 0.f, peak = 0.f;              // reference (log2 domain), sum; largest magnitude of a reference
       for (int j = 0; j < span.tiles; ++j) {
         const int k0 = span.tile(j) * kPaTile;
         if (!pa_valid(a, w0, it.P, k0)) continue;
@@ -308,6 +377,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         }
         if (first || move) m = top;
         const float b = m > -INFINITY ? -m : 0.f;
+        peak = fmaxf(peak, fabsf(b));
         tc::f32x2 sum[2] = {0ull, 0ull};
         {
           uint32_t p[32];
@@ -355,6 +425,13 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         }
       }
       if (a.lse && row < it.P) a.lse[(size_t)it.bh * a.P + row] = (m + log2f(l)) * 0.6931471805599453f;
+      const unsigned far = __ballot_sync(0xffffffffu, row < it.P && peak > kPaFar);
+      if (far) {
+        const size_t hk = (size_t)(it.b * a.Hkv + it.bh % a.Hq / (a.Hq / a.Hkv)) * a.P, hq = (size_t)it.bh * a.P;
+        __syncwarp();                                        // the rows' first outputs are written
+        pa_far_rows<T, D>((const T*)a.Q + hq * D, (const T*)a.K + hk * D, (const T*)a.V + hk * D, (T*)a.out + hq * D, a.lse ? a.lse + hq : nullptr, far, r0,
+                          a.window, a.n_sink);
+      }
     }
   }
   tc::fence_before_sync();

@@ -101,6 +101,63 @@ def test_large_logits(cuda_device, dtype):
         check(q[0, 0], k[0, 0], v[0, 0], out[0, 0], lse[0, 0], 0, 0, dtype)
 
 
+@pytest.mark.parametrize("dtype,scale", [("f16", 1000), ("f16", 8000), ("f16", 30000), ("bf16", 1000), ("bf16", 5e4), ("bf16", 1e9), ("bf16", 1e17), ("f32", 1e8)])
+@pytest.mark.parametrize("d,window,sinks", [(128, 0, 0), (64, 0, 0), (128, 100, 3)])
+def test_huge_logits(cuda_device, dtype, scale, d, window, sinks):
+    """Logits up to the largest that fp32 sums hold: a row is the value of its largest logit wherever that leads the next by more than the
+    logits' own error (2 delta of the tolerance) and by 40, and never NaN; beside them rows of ordinary size."""
+    n = 500
+    q, k, v = draw(n, 1, 2, 1, n, d, "f32")
+    limit = torch.finfo(DT[dtype]).max
+    q, k, v = ((t * scale).clamp(-limit, limit).to(DT[dtype]) for t in (q, k, v / scale))
+    q[:, :, ::7] = (q[:, :, ::7].float() / (float(scale) * scale)).to(DT[dtype])                       # logits of a few units
+    out, lse = torch.full_like(q, float("nan")), torch.empty(1, 2, n, device="cuda")
+    B.d2o_prompt_attention(q, k, v, out, lse=lse, window=window, n_sink=sinks)
+    assert bool(torch.isfinite(out.float()).all()) and bool(torch.isfinite(lse).all())
+    i, j = torch.arange(n, device="cuda")[:, None], torch.arange(n, device="cuda")[None]
+    seen = (j <= i) & ((j > i - window) | (j < sinks)) if window > 0 else j <= i
+    K, V = k[0, 0].double(), v[0, 0].double()
+    for h in range(2):
+        Q = q[0, h].double()
+        x = (Q @ K.T / math.sqrt(d)).masked_fill(~seen, -math.inf)
+        delta = 16 * 2.0 ** -24 * (Q.abs() @ K.abs().T / math.sqrt(d)).masked_fill(~seen, 0).amax(1)
+        two = x.topk(2, dim=1).values
+        clear = (two[:, 0] - two[:, 1] > 2 * delta + 40) | (torch.arange(n, device="cuda") == 0)
+        assert int(clear.sum()) > (300 if scale > 500 else 0)
+        # one weight of nearly 1: it is off by its own rounding against the sum, and the division by 2^-21
+        weights = 0.0 if dtype == "f32" else torch.finfo(DT[dtype]).eps / 2
+        one, o = V[x.argmax(1)][clear], out[0, h][clear].double()
+        e = (weights + 2.0 ** -21) * one.abs()
+        assert bool((((one - e).to(DT[dtype]).double() <= o) & (o <= (one + e).to(DT[dtype]).double())).all())
+        assert bool(((lse[0, h].double() - torch.logsumexp(x, 1)).abs()[clear] <= (delta + 2.0 ** -22 * two[:, 0].abs().clamp(min=1))[clear]).all())
+        small = torch.arange(0, n, 7, device="cuda")
+        p = torch.softmax(x[small], 1)
+        e = (weights + 2 * delta[small, None] + 2.0 ** -21) * (p @ V.abs())
+        ref, o = p @ V, out[0, h][small].double()
+        assert bool((((ref - e).to(DT[dtype]).double() <= o) & (o <= (ref + e).to(DT[dtype]).double())).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_huge_logits_come_and_go(cuda_device, dtype, d):
+    """References of -5e6 that give way to ordinary logits at key 200, and one key of +5e6 at 350: rows 200 .. 349 are those of a prompt without
+    the first 200 keys (delta from theirs alone), rows from 350 on are that key's value (see test_huge_logits)."""
+    n = 700
+    q, k, v = draw(21, 1, 1, 1, n, d, "f32")
+    q, k = q * 0.5, k * 0.5
+    q[..., 0], k[..., 0] = 8000.0, 0.0
+    k[:, :, :200, 0], k[:, :, 350, 0] = -8000.0, 8000.0
+    q, k, v = (t.to(DT[dtype]) for t in (q, k, v))
+    out, lse = torch.full_like(q, float("nan")), torch.empty(1, 1, n, device="cuda")
+    B.d2o_prompt_attention(q, k, v, out, lse=lse)
+    assert bool(torch.isfinite(out.float()).all()) and bool(torch.isfinite(lse).all())
+    check(q[0, 0, 200:350], k[0, 0, 200:350], v[0, 0, 200:350], out[0, 0, 200:350], lse[0, 0, 200:350], 0, 0, dtype)
+    weights = 0.0 if dtype == "f32" else torch.finfo(DT[dtype]).eps / 2
+    one, o = v[0, 0, 350].double(), out[0, 0, 350:].double()
+    e = (weights + 2.0 ** -21) * one.abs()
+    assert bool((((one - e).to(DT[dtype]).double() <= o) & (o <= (one + e).to(DT[dtype]).double())).all())
+
+
 def test_not_finite(cuda_device):
     """A NaN key reaches the rows that see it and no others; +inf and -inf logits give NaN and 0 as the formula does."""
     for dtype in DT:
