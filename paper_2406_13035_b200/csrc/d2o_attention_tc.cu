@@ -18,8 +18,8 @@
 // cycles against 2050 of products for both tiles; under load the power cap.  us: 32 / 8 heads of 32768 tokens under a window of 4096, bf16, 1800 cool and
 // 2190 warm (1.15 and 0.94 PFLOP/s); four ragged prompts of up to 6001 tokens 450 - 505; 32 heads of 1200 tokens 28.
 //
-// Rounding: weights to the input type for their product (relative half step 2^-9 bf16, 2^-12 fp16; the largest is 2^0 to 2^8, and
-// the errors of many keys average out); their sum and lse from the unrounded ones; S, O and all sums are fp32.
+// Rounding: weights to the input type for their product (relative half step 2^-8 bf16, 2^-11 fp16; the errors of many keys average out.
+// fp16 weights below 2^-21 of the row's largest are subnormal: off by up to 2^-32 of that, the most keys, 2^20, together by 2^-12); their sum and lse from the unrounded ones; S, O and all sums are fp32.
 #include <math.h>
 
 #include <cuda/std/type_traits>
@@ -35,6 +35,10 @@ constexpr int kPaTile = 128;
 constexpr int kPaSoftWarps = 8;
 constexpr int kPaThreads = (kPaSoftWarps + 4) * 32;          // three warpgroups: registers move between whole ones
 constexpr float kPaSlack = 8.f;              // growth of the maximum (log2 domain) that the reference leaves standing
+// How far below the maximum that it is set to the reference lies: the largest fp16 weight of a row is 2^7 to 2^15, so that nearly all of the
+// format's range lies below it.  (Four or two more, with as much less slack: 27.5 -> 28.2, 27.9 us for 32 heads of 1200 tokens, 57.0 -> 60.0, 58.9 for
+// two prompts of 2100.)
+template <int FMT> __host__ __device__ constexpr float pa_bias() { return FMT == 0 ? 7.f : 0.f; }
 constexpr float kPaFar = 1048576.f;          // references (log2 domain) beyond which their rounding is more than 1/16
 
 __host__ __device__ constexpr int pa_stages(int D) { return D == 128 ? 4 : 8; }
@@ -360,7 +364,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
           mx[2] = tc::max3(mx[2], __uint_as_float(s2[e]), __uint_as_float(s2[e + 1]));
           mx[3] = tc::max3(mx[3], __uint_as_float(s3[e]), __uint_as_float(s3[e + 1]));
         }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+        const float top = fmaf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), c, -pa_bias<FMT>());
         const bool first = m == -INFINITY, move = !first && top > m + kPaSlack;       // first: O (if any) and l are zero
         if (__any_sync(0xffffffffu, move)) {
           const float f = move ? tc::ex2(m - top) : 1.f;

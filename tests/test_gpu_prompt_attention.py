@@ -101,6 +101,38 @@ def test_large_logits(cuda_device, dtype):
         check(q[0, 0], k[0, 0], v[0, 0], out[0, 0], lse[0, 0], 0, 0, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("below", [18, 22, 24.4, 27.3, 30])
+def test_many_small_weights_beside_a_large_one(cuda_device, dtype, d, below):
+    """One key with nearly all of the weight and a value of nearly zero, and 20000 keys at 2^-below of it with values of one sign: what the small
+    weights lose in their rounding does not average out.  Beyond the tolerance of the other tests an fp16 weight below 2^-21 of the row's largest is off by
+    2^-32 of it (the largest is 2^7 at least, subnormals begin at 2^-14, and their half step is 2^-25)."""
+    n = 20000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k = (torch.zeros(1, 1, n, d, device="cuda") for _ in range(2))
+    v = 4 + torch.rand(1, 1, n, d, generator=g, device="cuda")
+    q[..., 0] = 4.0
+    k[:, :, 0, 0] = below * math.log(2) * math.sqrt(d) / 4
+    k[:, :, 1:, 1] = torch.randn(n - 1, generator=g, device="cuda")
+    v[:, :, 0] = 2.0 ** -20
+    q, k, v = (t.to(DT[dtype]) for t in (q, k, v))
+    out, lse = torch.empty_like(q), torch.empty(1, 1, n, device="cuda")
+    B.d2o_prompt_attention(q, k, v, out, lse=lse)
+    i = torch.tensor([1, 100, 5000, n - 1], device="cuda")
+    Q, K, V = q[0, 0, i].double(), k[0, 0].double(), v[0, 0].double()
+    x = (Q @ K.T / math.sqrt(d)).masked_fill(torch.arange(n, device="cuda")[None] > i[:, None], -math.inf)
+    p = torch.softmax(x, 1)
+    delta = 16 * 2.0 ** -24 * float((Q.abs() @ K.abs().T).max()) / math.sqrt(d)
+    e = ((0.0 if dtype == "f32" else torch.finfo(DT[dtype]).eps / 2) + 2 * delta + 2.0 ** -21) * (p @ V.abs())
+    if dtype == "f16":
+        e += 2.0 ** -32 * ((p > 0) * (p < 2.0 ** -21 * p.amax(1, keepdim=True))).double() @ V.abs() * p.amax(1, keepdim=True)
+    ref, o = p @ V, out[0, 0, i].double()
+    assert bool((((ref - e).to(DT[dtype]).double() <= o) & (o <= (ref + e).to(DT[dtype]).double())).all()), ((o - ref) / ref).abs().amax(1).tolist()
+    y = torch.logsumexp(x, 1)
+    assert bool(((lse[0, 0, i].double() - y).abs() <= delta + 2.0 ** -22 * y.abs().clamp(min=1)).all())
+
+
 @pytest.mark.parametrize("dtype,scale", [("f16", 1000), ("f16", 8000), ("f16", 30000), ("bf16", 1000), ("bf16", 5e4), ("bf16", 1e9), ("bf16", 1e17), ("f32", 1e8)])
 @pytest.mark.parametrize("d,window,sinks", [(128, 0, 0), (64, 0, 0), (128, 100, 3)])
 def test_huge_logits(cuda_device, dtype, scale, d, window, sinks):
