@@ -500,7 +500,9 @@ paged_decode_kernel(PagedDecodeArgs a) {
 // Every warp takes every twelfth (eighth) tile of its CTA's share, through a ring of its own in shared memory that tiled tensor maps fill (128-
 // byte swizzle; one lane asks for the tiles ahead, across slices): nothing waits for another warp but the end of a part.  Logits:
 // rows x heads = K q^T on m16n8k16 (the up to eight heads are the columns); outputs: d x heads = V^T P with the weights as two 16-bit
-// terms, so that they keep 16 (bf16) or 22 (fp16) bits.  Tiles at the edge of what is seen have their unseen value rows zeroed in shared
+// terms, so that they keep 16 (bf16) or 22 (fp16) bits.  The references m of fp16 weights 2^(x - m) lie 14 below the maximum: the largest
+// weight is 2^14, and those below 2^-16 of it, whose second term is subnormal, are off by up to 2^-39 of it (2^-25 with the
+// reference at the maximum, half a percent of a weight of 2^-17).  Tiles at the edge of what is seen have their unseen value rows zeroed in shared
 // memory (0 * NaN), and the new token's row put in its place.
 struct PagedMaps { CUtensorMap k, v; };
 
@@ -754,7 +756,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
       float w[4];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float mn = fmaxf(m[e], mx[e]), base = mn > -INFINITY ? mn : 0.f;
+        // rounded up: with huge logits the difference is not there, and must not be more
+        const float mn = fmaxf(m[e], cuda::std::is_same<T, __half>::value ? __fsub_ru(mx[e], 14.f) : mx[e]), base = mn > -INFINITY ? mn : 0.f;
         f[e] = exp2f(m[e] - base);                           // nothing so far: 0
         m[e] = mn;
         w[e] = exp2f(x[e] - base); w[e + 2] = exp2f(x[e + 2] - base);

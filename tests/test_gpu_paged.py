@@ -254,6 +254,71 @@ def test_decode_long(cuda_device, dtype):
     c.check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,G,room", [(64, 1, 0), (128, 4, 0), (128, 2, 40000)])
+@pytest.mark.parametrize("below", [14, 18, 22.3, 27, 31])
+def test_decode_many_small_weights_beside_a_large_one(cuda_device, dtype, d, G, room, below):
+    """One row with nearly all of the weight and a value of nearly zero, and 8000 rows at 2^-below of it with values of one sign: what the small weights
+    lose in their rounding does not average out.  Beyond the tolerance of the other tests an fp16 weight below 2^-16 of the row's largest is off by
+    2^-39 of it (the largest is 2^14; the second term's half step is 2^-25 where it is subnormal), and the fp32 sum over the rows of a warp grows by
+    one product of 16 rows, of two terms each, at a time, each off by up to a unit in its last place (2^-23; 8000 rows over at least eight warps: 63 products)."""
+    n, page = 8000, 16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    per = n // page + 1
+    table = torch.full((1, max(per, room // page)), -1, dtype=torch.int32, device="cuda")
+    table[0, :per] = torch.randperm(per, generator=g, device="cuda")
+    K = torch.zeros(per * page, d, device="cuda")
+    V = 4 + torch.rand(per * page, d, generator=g, device="cuda")
+    K[0, 0], V[0] = below * math.log(2) * math.sqrt(d) / 4, 2.0 ** -20
+    K[1:, 1] = torch.randn(per * page - 1, generator=g, device="cuda")
+    q = torch.zeros(1, G, d, device="cuda")
+    q[..., 0] = 4.0
+    K, V, q = (t.to(DT[dtype]) for t in (K, V, q))
+    kp, vp = (torch.empty(per, 1, page, d, dtype=DT[dtype], device="cuda") for _ in range(2))
+    kp[table[0, :per].long()], vp[table[0, :per].long()] = K.view(per, 1, page, d), V.view(per, 1, page, d)
+    pos, score = torch.zeros(per, 1, page, dtype=torch.int32, device="cuda"), torch.zeros(per, 1, page, device="cuda")
+    c = B.D2OPagedCache(kp, vp, table, torch.full((1, 1), n - 1, dtype=torch.int32, device="cuda"), n_q_heads=G, pos=pos, score=score)
+    out = torch.empty_like(q)
+    c.d2o_paged_decode_step(q, K[None, None, n - 1].contiguous(), V[None, None, n - 1].contiguous(), out)
+    c.check()
+    Q, Kd, Vd = q[0].double(), K[:n].double(), V[:n].double()
+    x = Q @ Kd.T / math.sqrt(d)
+    p = torch.softmax(x, 1)
+    delta = 16 * 2.0 ** -24 * float((Q.abs() @ Kd.abs().T).max()) / math.sqrt(d)
+    w = 2 * delta + 2.0 ** -20
+    mag = p @ Vd.abs()
+    e = (w + (2.0 ** -16 if dtype == "bf16" else 0) + 2 * 63 * 2.0 ** -23) * mag
+    if dtype == "f16":
+        e += 2.0 ** -39 * p.amax(1, keepdim=True) * ((p < 2.0 ** -16 * p.amax(1, keepdim=True)).double() @ Vd.abs())
+    ref, o = p @ Vd, out[0].double()
+    assert bool((((ref - e).to(DT[dtype]).double() <= o) & (o <= (ref + e).to(DT[dtype]).double())).all()), ((o - ref) / ref).abs().amax().item()
+    got = score[table[0, :per].long()].flatten()[:n].double()
+    assert bool(((got - p.sum(0)).abs() <= (w + 2.0 ** -24) * p.sum(0)).all())
+
+
+@pytest.mark.parametrize("dtype,scale", [("f32", 1e9), ("f16", 300), ("f16", 3000), ("f16", 12000), ("f16", 30000), ("bf16", 3000), ("bf16", 1e9), ("bf16", 1e17)])
+@pytest.mark.parametrize("d,G", [(64, 1), (128, 4)])
+def test_decode_huge_logits(cuda_device, dtype, scale, d, G):
+    """Logits up to the largest that fp32 sums hold: the value of the row with the largest, exactly, where that leads the next by more than the
+    logits' own error and by 100, so that every other weight is zero beside it."""
+    c = Paged(31, 1, G, 1, d, dtype, 16, 20, [300], scored=False)
+    limit = torch.finfo(DT[dtype]).max
+    big = lambda t: (t.float() * scale).clamp(-limit, limit).to(DT[dtype])
+    c.k.copy_(big(c.k))
+    c.upload()
+    q, k, v = big(c.randn(1, G, d)), big(c.randn(1, 1, d)), c.randn(1, 1, d)
+    out = torch.full((1, G, d), 3.0, dtype=c.dt, device="cuda")
+    c.cache.d2o_paged_decode_step(q.cuda(), k.cuda(), v.cuda(), out)
+    K = torch.cat([c.rows(c.k, 0, 0, range(300)), k[0]]).double()
+    V = torch.cat([c.rows(c.v, 0, 0, range(300)), v[0]])
+    Q = q[0].double()
+    x = Q @ K.T / math.sqrt(d)
+    delta = 16 * 2.0 ** -24 * (Q.abs() @ K.abs().T / math.sqrt(d)).amax(1)
+    two = x.topk(2, dim=1).values
+    clear = two[:, 0] - two[:, 1] > 2 * delta + 100
+    assert bool(clear.any()) and torch.equal(out[0].cpu()[clear], V[x.argmax(1)][clear]) and bool(torch.isfinite(out.float()).all())
+
+
 def test_decode_offsets_past_32_bits(cuda_device):
     """A pool of more than 2^31 elements, and rows of it behind that border."""
     page, d, hkv, dt = 1024, 128, 8, torch.bfloat16
