@@ -298,8 +298,8 @@ d2o_status d2o_layer_stats_static(int32_t dtype, int32_t d_head, int32_t batch, 
  * d2o_layer_stats takes where window is 0), may be NULL; lens DEVICE int32 [B], the length of every sequence (0 ..
  * prompt_len), may be NULL: all prompt_len.  Rows of Q, K and V at and behind a sequence's length are padding: they may hold
  * anything, and those of out and lse stay as they were.  A length outside 0 .. prompt_len counts as the nearer end.
- * Inside a sequence a value that is not finite reaches the rows that see it, and may reach rows of the same 256 queries that do
- * not (0 * inf).
+ * Inside a sequence a value that is not finite reaches the rows that see it, and may make NaN of others in a block of 256 queries
+ * (0 .. 255, 256 .. 511, ...) of which one sees it (0 * inf); a key that is not finite reaches the rows that see it alone.
  * 16-bit inputs run on the tensor cores, the weights p rounded to the input type for their product with V (a relative half step of
  * 2^-8 bf16, 2^-11 fp16; fp16 weights below 2^-21 of the row's largest by up to 2^-32 of that; sums and lse from the unrounded weights); fp32 inputs on CUDA cores, in fp32 throughout.
  * status DEVICE uint32 [2], may be NULL: error word and detail (D2O_ERR_TIMEOUT: a device-side wait ran out; the rows of every thread

@@ -126,6 +126,13 @@ prompt_attention_kernel(PromptAttentionArgs a) {
       for (int e = 0; e < CD; ++e) acc[i][e] *= old;
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (k0 < span.lo) {      // values between the sinks and the first query's window, which no query of the tile sees, may be anything, and 0 * NaN is NaN
+#pragma unroll
+      for (int i = 0; i < V4; ++i) {
+        const int x = tid + i * kAttGroup, r = k0 + x / (D / 4);
+        if (r >= a.n_sink && r < span.lo) *reinterpret_cast<float4*>(sV + x * 4) = make_float4(0.f, 0.f, 0.f, 0.f);      // this thread's copy
+      }
+    }
     sync();
 #pragma unroll 2
     for (int j = 0; j < kAttTile; j += 4) {

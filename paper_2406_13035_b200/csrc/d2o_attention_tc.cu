@@ -285,12 +285,15 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         const int k0 = span.tile(j) * kPaTile;
         const bool next = j + 1 < n && pa_valid(a, w0, it.P, span.tile(j + 1) * kPaTile);
         if (!full(ring)) break;
-        if (k0 + kPaTile > it.P && now) {
-          // values behind the sequence's end may be anything, and 0 * NaN is NaN: zero them (both warps may: the same zeros)
-          for (int x = lane; x < (k0 + kPaTile - it.P) * KB * 8; x += 32) {
-            const int r = it.P - k0 + x / (KB * 8), piece = x % (KB * 8);
-            *reinterpret_cast<uint4*>(sKV + ring % STAGES * TILE + piece / 8 * BLOCK + r * 128 + piece % 8 * 16) = make_uint4(0, 0, 0, 0);
-          }
+        // Values that no query of the item sees may be anything, and 0 * NaN is NaN: those behind the sequence's end, and between the sinks and
+        // the first query's window, are zeroed.  The former by both warps (the same zeros), the latter by the first, which sees those tiles,
+        // ahead of its turn and so of the second's.
+        const bool end = k0 + kPaTile > it.P;
+        if (now && (end || (t == 0 && k0 < span.lo))) {
+          const int z0 = end ? it.P - k0 : max(0, a.n_sink - k0), z1 = end ? kPaTile : min(kPaTile, span.lo - k0), piece = lane % (KB * 8);
+          unsigned char* row = sKV + ring % STAGES * TILE + piece / 8 * BLOCK + piece % 8 * 16;
+#pragma unroll 4
+          for (int r = z0 + lane / (KB * 8); r < z1; r += 32 / (KB * 8)) *reinterpret_cast<uint4*>(row + r * 128) = make_uint4(0, 0, 0, 0);
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }

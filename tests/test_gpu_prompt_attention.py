@@ -209,6 +209,33 @@ def test_not_finite(cuda_device):
         assert bool(torch.isfinite(out[0, 0, :500].float()).all()) and bool(out[0, 0, 500:].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n,window,sinks,at", [(1000, 200, 0, 0), (1000, 200, 0, 56), (1000, 200, 4, 4), (1000, 200, 4, 50), (1500, 130, 200, 200), (1500, 130, 200, 255),
+                                               (900, 64, 0, 300), (900, 300, 3, 700), (700, 0, 0, 600), (2000, 257, 129, 511), (800, 1, 0, 255), (1300, 128, 5, 127)])
+def test_values_that_are_not_finite(cuda_device, dtype, d, n, window, sinks, at):
+    """An infinite or NaN value reaches the rows that see its key, and of the others those in a block of 256 queries of which one sees it at most; a
+    key that is not finite the rows that see it alone."""
+    q, k, v = draw(n + at, 1, 2, 1, n, d, dtype)
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    B.d2o_prompt_attention(q, k, v, want, window=window, n_sink=sinks)
+    i = torch.arange(n, device="cuda")
+    sees = (i >= at) & ((i < at + window) | (at < sinks)) if window else i >= at
+    blocks = torch.zeros(-(-n // 256), dtype=torch.bool, device="cuda")
+    blocks[i[sees] // 256] = True
+    apart = ~blocks[i // 256]
+    for bad in (math.inf, -math.inf, math.nan):
+        x = v.clone()
+        x[0, 0, at] = bad
+        B.d2o_prompt_attention(q, k, x, out, window=window, n_sink=sinks)
+        assert bool((~torch.isfinite(out[:, :, sees].float())).all())
+        assert torch.equal(out[:, :, apart], want[:, :, apart])
+        x = k.clone()
+        x[0, 0, at] = math.nan
+        B.d2o_prompt_attention(q, x, v, out, window=window, n_sink=sinks)
+        assert bool(out[:, :, sees].isnan().all()) and torch.equal(out[:, :, ~sees], want[:, :, ~sees])
+
+
 def test_normalisers_feed_the_column_sums(cuda_device):
     """lse as d2o_layer_stats takes it: the same column sums, to rounding, as with its own first sweep."""
     q, k, v = draw(3, 1, 8, 2, 777, 128, "bf16")
