@@ -364,7 +364,8 @@ d2o_status d2o_paged_append(const d2o_paged_cache* cache, int32_t n_rows, const 
  * case 2).  A sequence whose table does not reach row t gets NaN outputs, and one that
  * has a bad page number among the rows seen NaN outputs and scores, in the heads concerned; both set the error word.  So does a
  * device-side wait that runs out (D2O_ERR_TIMEOUT), with NaN outputs and scores in the heads concerned, whose new row may not have been
- * written.  Rows outside the view may hold anything.  The caller adds one to len.
+ * written.  Rows outside the view may hold anything.  A row seen whose value is infinite gives infinity in the outputs concerned, or NaN
+ * where its weight vanishes (16-bit caches: below 2^-27 of the largest).  The caller adds one to len.
  * The rows of all sequences together are divided evenly over the GPU, whatever the single lengths, and what was divided is
  * joined again in a fixed order: results do not change from run to run.  Asynchronous. */
 d2o_status d2o_paged_decode_step(const d2o_paged_cache* cache, int32_t window, int32_t n_sink, const void* q, const void* k,

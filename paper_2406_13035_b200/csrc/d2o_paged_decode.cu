@@ -512,6 +512,22 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
   return y;
 }
 
+// Two weights as 16-bit terms, hi strictly below a weight that is not zero and lo the rest, rounded: both positive, so that an infinite value gives
+// infinity (0 * inf would be NaN, and so would the sum with a negative second term).  fp16: down to weights of 2^-13, below which lo may round to zero.
+template <typename T>
+__device__ __forceinline__ void split_below(float x, float y, uint32_t& hi, uint32_t& lo) {
+  const uint32_t xb = __float_as_uint(x), yb = __float_as_uint(y), xd = xb - min(xb, 1u), yd = yb - min(yb, 1u);
+  if constexpr (cuda::std::is_same<T, __nv_bfloat16>::value) {
+    hi = __byte_perm(xd, yd, 0x7632);                        // the upper halves
+    const __nv_bfloat162 l = __floats2bfloat162_rn(x - __uint_as_float(xd & 0xffff0000u), y - __uint_as_float(yd & 0xffff0000u));
+    lo = *reinterpret_cast<const uint32_t*>(&l);
+  } else {
+    const __half xh = __float2half_rz(__uint_as_float(xd)), yh = __float2half_rz(__uint_as_float(yd));
+    const __half2 h = __halves2half2(xh, yh), l = __floats2half2_rn(x - __half2float(xh), y - __half2float(yh));
+    hi = *reinterpret_cast<const uint32_t*>(&h); lo = *reinterpret_cast<const uint32_t*>(&l);
+  }
+}
+
 // A warp's place in the tiles of its CTA: tile `at` of all, in slice `sl`, which begins at tile `before`.
 struct PagedCursor {
   long long at, before;
@@ -768,8 +784,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
         for (int i = 0; i < D / 16; ++i) { acc[i][0] *= f[0]; acc[i][1] *= f[1]; acc[i][2] *= f[0]; acc[i][3] *= f[1]; }
       }
       uint32_t h0, l0, h1, l1;
-      split_pair<T>(w[0], w[1], h0, l0);
-      split_pair<T>(w[2], w[3], h1, l1);
+      split_below<T>(w[0], w[1], h0, l0);
+      split_below<T>(w[2], w[3], h1, l1);
       h0 = transpose_8x8(h0); h1 = transpose_8x8(h1); l0 = transpose_8x8(l0); l1 = transpose_8x8(l1);
       const uint32_t v_u32 = smem_u32(stage + TILE);
 #pragma unroll

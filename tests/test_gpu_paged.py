@@ -319,6 +319,53 @@ def test_decode_huge_logits(cuda_device, dtype, scale, d, G):
     assert bool(clear.any()) and torch.equal(out[0].cpu()[clear], V[x.argmax(1)][clear]) and bool(torch.isfinite(out.float()).all())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d,G", [(64, 1), (128, 4), (64, 8), (128, 2)])
+@pytest.mark.parametrize("n,room", [(5, 16), (300, 320), (2000, 2016), (2000, 60000)])
+def test_decode_rows_that_are_not_finite(cuda_device, dtype, d, G, n, room):
+    """Rows that are seen: infinite values give infinities, of both signs or NaN ones NaN, in those elements alone; a logit of -inf a weight of zero, a
+    NaN one NaN in the heads of its slice.  Weights are within 2^-20 of the largest."""
+    page, hkv = 16, 3
+    g = torch.Generator(device="cuda").manual_seed(n + d + G)
+    per = n // page + 1
+    table = torch.full((1, room // page + 1), -1, dtype=torch.int32, device="cuda")
+    table[0, :per] = torch.randperm(per, generator=g, device="cuda")
+    at = lambda r: (int(table[0, r // page]), r % page)
+    kp, vp = (torch.randn(per, hkv, page, d, generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    q, k, v = (torch.randn(1, h, d, generator=g, device="cuda").to(DT[dtype]) for h in (hkv * G, hkv, hkv))
+    kp[..., 5], k[..., 5], q[..., 5] = 0.0, 0.0, 1.0
+    pos, score = torch.zeros(per, hkv, page, dtype=torch.int32, device="cuda"), torch.zeros(per, hkv, page, device="cuda")
+    c = B.D2OPagedCache(kp, vp, table, torch.full((1, hkv), n, dtype=torch.int32, device="cuda"), n_q_heads=hkv * G, pos=pos, score=score)
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    c.d2o_paged_decode_step(q, k, v, want)
+    rows = [0, n // 3, n - 1]
+    for r, e, x in [(rows[0], 1, math.inf), (rows[1], 2, -math.inf), (rows[2], 3, math.nan), (rows[0], 4, math.inf), (rows[2], 4, -math.inf), (rows[1], 9, math.inf), (rows[2], 9, math.inf)]:
+        vp[at(r)[0], 0, at(r)[1], e] = x
+    vn = v.clone()
+    vn[0, 0, 7] = -math.inf                                                    # the new token's own
+    kp[at(rows[1])[0], 1, at(rows[1])[1], 5] = -math.inf
+    kp[at(rows[2])[0], 2, at(rows[2])[1], 5] = math.nan
+    score.zero_()
+    c.d2o_paged_decode_step(q, k, vn, out)
+    c.check()
+    o = out[0].view(hkv, G, d)
+    first = o[0].float()
+    assert bool((first[:, [1, 9]] == math.inf).all()) and bool((first[:, [2, 7]] == -math.inf).all()) and bool(first[:, [3, 4]].isnan().all())
+    rest = [e for e in range(d) if e not in (1, 2, 3, 4, 7, 9)]
+    assert torch.equal(first[:, rest], want[0].view(hkv, G, d)[0].float()[:, rest])
+    assert bool(o[2].isnan().all())
+    # slice 1: as without that row
+    keep = [r for r in range(n) if r != rows[1]]
+    line = lambda pool, h: pool[table[0, :per].long(), h].flatten(0, 1)
+    K, V, Q = torch.cat([line(kp, 1)[keep], k[0, 1:2]]).double(), torch.cat([line(vp, 1)[keep], v[0, 1:2]]).double(), q[0, G:2 * G].double()
+    p = torch.softmax(Q @ K.T / math.sqrt(d), -1)
+    w = 32 * 2.0 ** -24 * float((Q.abs() @ K.abs().T).max()) / math.sqrt(d) + 2.0 ** -20
+    e, ref = (w + (2.0 ** -16 if dtype == "bf16" else 0)) * (p @ V.abs()), p @ V
+    assert bool((((ref - e).to(DT[dtype]).double() <= o[1].double()) & (o[1].double() <= (ref + e).to(DT[dtype]).double())).all())
+    assert float(score[at(rows[1])[0], 1, at(rows[1])[1]]) == 0.0
+    assert bool((line(score, 1)[:n + 1][keep] > 0).all()) and bool(line(score, 2)[:n + 1].isnan().all()) and bool(torch.isfinite(line(score, 0)[:n + 1]).all())
+
+
 def test_decode_offsets_past_32_bits(cuda_device):
     """A pool of more than 2^31 elements, and rows of it behind that border."""
     page, d, hkv, dt = 1024, 128, 8, torch.bfloat16
