@@ -256,7 +256,7 @@ evict_kernel(EvictArgs a) {
     sync_all();                                              // our exchange area may still be read
     return;
   }
-  auto inverse_pos = [&](int i) { return ~(uint32_t)p.pos[pool_row(r0 + i)]; };
+  auto inverse_pos = [&](int i) { return (uint32_t)p.pos[pool_row(r0 + i)] ^ 0x7fffffffu; };      // falls as the position, of either sign, grows
   EvictExchange* const lead_x = CL ? cluster.map_shared_rank(&x, 0) : &x;
   auto gather = [&](unsigned long long v) {                  // to the first CTA's list: in_bin rows
     const int at = atomicAdd(&lead_x->few, 1);

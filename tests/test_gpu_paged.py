@@ -556,6 +556,22 @@ def test_evict(cuda_device, b, hq, hkv, d, dtype, page, held, budget, window, si
     c.cache.check()
 
 
+@pytest.mark.parametrize("held,budget", [(40, 9), (90, 25), (700, 15), (2000, 1100)])
+def test_evict_positions_below_zero(cuda_device, held, budget):
+    """Positions around zero, as a padded batch may count them: all below n_sink are protected, and the budget is spent on the earliest of them; and ties
+    of ordinary rows on both sides of zero."""
+    c = Paged(held, 2, 4, 2, 64, "bf16", 16, (held + 15) // 16, [held, held - 1])
+    c.pos.copy_(torch.where(c.pos == -7, c.pos, c.pos - 17))
+    c.score.copy_(torch.where(c.score == c.score, (c.score * 2).floor(), c.score))
+    c.upload()
+    budgets = torch.tensor([[budget, budget + 1], [budget - 1, 7]], dtype=torch.int32)
+    next_pos = torch.tensor([held - 17, held - 18], dtype=torch.int32)
+    c.cache.d2o_paged_evict(budgets.cuda(), next_pos.cuda(), n_sink=5, window=3)
+    c.evict(budgets, next_pos, 5, 3)
+    c.same()
+    c.cache.check()
+
+
 @pytest.mark.parametrize("n,budget,b,hkv", [(30000, 6000, 1, 8), (30001, 29990, 1, 1), (20000, 3000, 40, 8)])
 def test_evict_long(cuda_device, n, budget, b, hkv):
     """More rows than shared memory keeps keys of, ties at the border; checked on the GPU."""
