@@ -484,6 +484,64 @@ def test_streams_at_once(cuda_device):
         assert torch.equal(a[4], want[0]) and torch.equal(b[4], want[1]) and torch.equal(o, want[2])
 
 
+def test_scores_and_evictions_on_streams_at_once(cuda_device):
+    """Two caches with scores that take steps, one of them between evictions, a third that is evicted from, and a prompt's attention, on four streams
+    at the same time, many times over: the bits of the same calls one after another."""
+    a = _batch(11, 20, 8, 4, 128, "bf16", 16, 1500, True)
+    b = _batch(12, 3, 8, 1, 64, "f32", 32, 4000, True)
+    e = _batch(13, 5, 8, 2, 128, "f16", 16, 9000, True)
+    Q, K, V = (torch.randn(2, h, 700, 128, device="cuda").half() for h in (8, 2, 2))
+    o = torch.empty_like(Q)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for x in (a, b, e):
+        pos, score = x[0].tensors[4:6]
+        pos.copy_(torch.randint(0, 1 << 20, pos.shape, generator=g, device="cuda"))
+        score.copy_(torch.rand(score.shape, generator=g, device="cuda"))
+    pools = [[x[0].tensors[j] for j in (0, 1, 4, 5)] for x in (a, b, e)]
+    kept = [[t.clone() for t in ts] for ts in pools]
+    next_pos = {id(x): torch.full((x[0].shape[0],), 1 << 19, dtype=torch.int32, device="cuda") for x in (a, b, e)}
+    budgets = {id(x): (x[0].tensors[3] // 3).contiguous() for x in (a, b, e)}
+
+    def steps(x):
+        for _ in range(3):
+            x[0].d2o_paged_decode_step(x[1], x[2], x[3], x[4])
+
+    def evict(x):
+        x[0].d2o_paged_evict(budgets[id(x)], next_pos[id(x)], n_sink=100, window=50)
+
+    def between():
+        steps(a)
+        evict(a)
+        steps(a)
+    jobs = [between, lambda: steps(b), lambda: evict(e), lambda: B.d2o_prompt_attention(Q, K, V, o, window=100, n_sink=2)]
+    results = lambda: [t for ts in pools for t in ts] + [a[4], b[4], o]
+
+    def restore():
+        for ts, ks in zip(pools, kept):
+            for t, k in zip(ts, ks):
+                t.copy_(k)
+        for t in (a[4], b[4], o):
+            t.zero_()
+        torch.cuda.synchronize()
+    restore()
+    for job in jobs:
+        job()
+        torch.cuda.synchronize()
+    want = [t.clone() for t in results()]
+    assert not torch.equal(want[2], kept[0][2]) and not torch.equal(want[10], kept[2][2])      # evictions moved rows
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for turn in range(12):
+        restore()
+        for i in range(4):
+            with torch.cuda.stream(streams[(i + turn) % 4]):
+                jobs[(i + turn) % 4]()
+        torch.cuda.synchronize()
+        for t, w in zip(results(), want):
+            assert np.array_equal(bits(t), bits(w))
+    for x in (a, b, e):
+        x[0].check()
+
+
 def test_made_on_one_stream_used_on_another(cuda_device):
     """The scratch is cleared when the constructor returns, also behind work that is under way on its stream."""
     a = _batch(3, 20, 8, 4, 128, "bf16", 16, 1500)
@@ -518,6 +576,33 @@ def test_one_scratch_for_several_caches(cuda_device):
             check(out, [(i, i % hkv) for i in range(0, b, max(1, b // 8))])
             c.d2o_paged_evict((c.tensors[3] + 1).contiguous(), torch.full((b,), 30000, dtype=torch.int32, device="cuda"))     # nothing to do
             c.check()
+
+
+def test_steps_and_evictions_of_several_caches_on_one_scratch(cuda_device):
+    """Steps with scores and evictions that move rows, of caches of other shapes in turn, through one scratch (the logits of one lie where the moves of the
+    other do): every pool against the plain statements."""
+    shapes = [(2, 4, 2, 64, "bf16", 16, [90, 61]), (1, 8, 1, 128, "f16", 32, [200]), (3, 2, 2, 64, "f32", 16, [40, 75, 3])]
+    caches = [Paged(i, b, hq, hkv, d, dt, page, max(held) // page + 2, held) for i, (b, hq, hkv, d, dt, page, held) in enumerate(shapes)]
+    big = max((c.cache for c in caches), key=lambda c: c._scratch[1])
+    for c in caches:
+        c.cache._scratch = big._scratch
+    for turn in range(3):
+        for c in caches:
+            q, k, v = c.randn(c.b, c.hq, c.d), c.randn(c.b, c.hkv, c.d), c.randn(c.b, c.hkv, c.d)
+            out = torch.full((c.b, c.hq, c.d), 3.0, dtype=c.dt, device="cuda")
+            c.cache.d2o_paged_decode_step(q.cuda(), k.cuda(), v.cuda(), out)
+            c.step(q, k, v, out, None, 0, 0)
+            c.same()
+            c.len += 1
+            c.dlen.copy_(c.len)
+        for c in caches:
+            budgets, next_pos = (c.len * 2 // 3).to(torch.int32), c.len.amax(1).to(torch.int32)
+            c.cache.d2o_paged_evict(budgets.cuda(), next_pos.cuda(), n_sink=1, window=5)
+            c.evict(budgets, next_pos, 1, 5)
+            c.same()
+            c.len = torch.minimum(c.len, budgets)
+            c.dlen.copy_(c.len)
+            c.cache.check()
 
 
 # ---------------------------------------------------------------------------------------------- evict

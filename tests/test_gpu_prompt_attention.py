@@ -87,6 +87,23 @@ def test_ragged(cuda_device, lens, window, sinks, dtype):
             check(q[i, h, :m], k[i, h // 2, :m], v[i, h // 2, :m], out[i, h, :m], None, window, sinks, dtype)
 
 
+@pytest.mark.parametrize("dtype,d", [("f16", 128), ("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("b,hq,hkv,n,window,sinks", [(2, 96, 8, 1100, 0, 0), (2, 96, 8, 1100, 300, 4), (5, 40, 40, 800, 0, 0), (5, 40, 40, 800, 150, 200)])
+def test_more_blocks_than_places(cuda_device, dtype, d, b, hq, hkv, n, window, sinks):
+    """Several blocks of queries for every SM, each of several tiles of keys and of lengths of their own, so that thread blocks go on with the work of others
+    in every state of their rings."""
+    q, k, v = draw(n + b, b, hq, hkv, n, d, dtype)
+    lens = torch.tensor([n, n // 2 + 30, 1, n - 129, 257][:b], dtype=torch.int32)
+    out, lse = torch.full_like(q, 7.0), torch.full((b, hq, n), 7.0, device="cuda")
+    status = torch.zeros(2, dtype=torch.int32, device="cuda")
+    B.d2o_prompt_attention(q, k, v, out, lse=lse, window=window, n_sink=sinks, lens=lens.cuda(), status=status)
+    for i, m in enumerate(lens.tolist()):
+        assert bool((out[i, :, m:] == 7).all()) and bool((lse[i, :, m:] == 7).all())
+        for h in range(hq):
+            check(q[i, h, :m], k[i, h * hkv // hq, :m], v[i, h * hkv // hq, :m], out[i, h, :m], lse[i, h, :m], window, sinks, dtype)
+    assert status.tolist() == [0, 0]
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_large_logits(cuda_device, dtype):
     """Logits in the hundreds that grow along the row, so that the running maximum moves in every tile, and fall, so that it never
