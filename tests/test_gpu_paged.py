@@ -641,6 +641,38 @@ def test_evict(cuda_device, b, hq, hkv, d, dtype, page, held, budget, window, si
     c.cache.check()
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 128), ("f16", 64)])
+@pytest.mark.parametrize("held,budget", [([1, 0], [0, 0]), ([5, 300], [3, 41]), ([17, 16], [16, 15]), ([2, 40], [1, 39]), ([600, 1500], [1, 1499])])
+def test_evict_few_rows_in_a_large_table(cuda_device, dtype, d, held, budget):
+    """Tables with room for 33600 rows: clusters of sixteen, most of whose CTAs have no rows."""
+    c = Paged(sum(held) + d, 2, 4, 2, d, dtype, 16, 2100, held)
+    c.score.copy_(torch.where(c.score == c.score, (c.score * 6).floor(), c.score))
+    c.table[:, (max(held) + 15) // 16:] = -1
+    c.upload()
+    budgets = torch.tensor(budget, dtype=torch.int32)[:, None].expand(2, 2).contiguous()
+    next_pos = torch.tensor(held, dtype=torch.int32)
+    c.cache.d2o_paged_evict(budgets.cuda(), next_pos.cuda(), n_sink=1, window=9)
+    c.evict(budgets, next_pos, 1, 9)
+    c.same()
+    c.cache.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("b,max_pages", [(2, 4), (2, 4000), (700, 4)])
+def test_no_sequences(cuda_device, dtype, b, max_pages):
+    """A batch of padding alone: nothing is read or written."""
+    c = Paged(3, b, 4, 2, 64, dtype, 16, max_pages, [-1] * b)
+    out = torch.full((b, 4, 64), 3.0, dtype=c.dt, device="cuda")
+    x = lambda *s: torch.zeros(*s, dtype=c.dt, device="cuda")
+    for _ in range(2):
+        c.cache.d2o_paged_decode_step(x(b, 4, 64), x(b, 2, 64), x(b, 2, 64), out)
+        c.cache.d2o_paged_append(x(b, 2, 5, 64), x(b, 2, 5, 64))
+        c.cache.d2o_paged_evict(torch.zeros(b, 2, dtype=torch.int32, device="cuda"), torch.zeros(b, dtype=torch.int32, device="cuda"))
+    assert bool((out == 3).all())
+    c.same()
+    c.cache.check()
+
+
 @pytest.mark.parametrize("held,budget", [(40, 9), (90, 25), (700, 15), (2000, 1100)])
 def test_evict_positions_below_zero(cuda_device, held, budget):
     """Positions around zero, as a padded batch may count them: all below n_sink are protected, and the budget is spent on the earliest of them; and ties
