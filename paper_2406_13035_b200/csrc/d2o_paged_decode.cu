@@ -244,7 +244,7 @@ struct PagedOpen {
 // The warps' results of one part (tiles i0 .. i1 of slice `sl`) become the slice's output, or one of the parts to be joined.  s_m, s_l:
 // maxima and sums [warps][ld]; the maxima become the warps' factors.  CL: a part for join_cluster, in shared memory.  Begins and ends behind a barrier of the caller's.
 template <typename T, int D, int G, int LD, bool CL>
-__device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, const PagedStart& start, PagedOpen& open, float* swap, int part, int sl, int i0, int i1,
+__device__ __forceinline__ void finish_part(const PagedDecodeArgs& a, PagedOpen& open, float* swap, int part, int sl, int i0, int i1,
                                             const PagedSpan& span, long long before, const float* red, float* s_m, float* s_l, int ld) {
   const PagedView& p = a.p;
   const int tid = threadIdx.x, c = blockIdx.x, b = sl / p.Hkv, h = sl % p.Hkv;
@@ -487,7 +487,7 @@ paged_decode_kernel(PagedDecodeArgs a) {
       }
     }
     __syncthreads();
-    finish_part<T, D, G, D, CL>(a, start, open, swap, i1 < span.tiles ? 1 : 0, sl, i0, i1, span, before, red, &s_m[0][0], &s_l[0][0], G);
+    finish_part<T, D, G, D, CL>(a, open, swap, i1 < span.tiles ? 1 : 0, sl, i0, i1, span, before, red, &s_m[0][0], &s_l[0][0], G);
     __syncthreads();                                         // before the exchange area is written again
     at = before + i1;
     before += span.tiles;
