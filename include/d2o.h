@@ -296,7 +296,7 @@ d2o_status d2o_layer_stats_static(int32_t dtype, int32_t d_head, int32_t batch, 
  *
  * Q and out DEVICE [B, Hq, P, d], K and V DEVICE [B, Hkv, P, d] in `dtype`; lse DEVICE float [B, Hq, P], natural log (what
  * d2o_layer_stats takes where window is 0), may be NULL; lens DEVICE int32 [B], the length of every sequence (0 ..
- * prompt_len), may be NULL: all prompt_len.  Rows of Q, K and V at and behind a sequence's length are padding: they may hold
+ * prompt_len), may be NULL: all prompt_len.  out and lse overlap none of the inputs.  Rows of Q, K and V at and behind a sequence's length are padding: they may hold
  * anything, and those of out and lse stay as they were.  A length outside 0 .. prompt_len counts as the nearer end.
  * Inside a sequence a value that is not finite reaches the rows that see it, and may make NaN of others in a block of 256 queries
  * (0 .. 255, 256 .. 511, ...) of which one sees it (0 * inf); a key that is not finite reaches the rows that see it alone.
@@ -359,7 +359,7 @@ d2o_status d2o_paged_append(const d2o_paged_cache* cache, int32_t n_rows, const 
 /* One generated token per sequence (Eq. 2-3): (k, v) goes to row t = len[b, h], and the query heads of h attend over the rows
  * r <= t, with window > 0 only r > t - window or r < n_sink.  Rows count in the order in which they lie in the pages: a cache
  * that d2o_paged_evict has been through is no longer in the order of positions, so that a window has no meaning there.
- * q, out DEVICE [B, Hq, d]; k, v DEVICE [B, Hkv, d].  With pos and score: row t gets positions[b] (DEVICE int32 [B]; NULL: t),
+ * q, out DEVICE [B, Hq, d]; k, v DEVICE [B, Hkv, d]; no input overlaps out or the pages.  With pos and score: row t gets positions[b] (DEVICE int32 [B]; NULL: t),
  * its weight, summed over the query heads, as score, and every other row that is seen has its weight added to its score (Eq. 6
  * case 2).  A sequence whose table does not reach row t gets NaN outputs, and one that
  * has a bad page number among the rows seen NaN outputs and scores, in the heads concerned; both set the error word.  So does a

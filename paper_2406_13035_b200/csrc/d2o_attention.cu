@@ -2,10 +2,10 @@
 //
 // One CTA per 64 queries of a head; keys and values in tiles of 64, which two groups of 256 threads take in turns, each with a running
 // maximum, sum and output of its own, joined at the end: twice the warps where a prompt has few CTAs (8 heads of 1024 tokens, d = 64,
-// window 256: 46 us with one group, 30.5 with two, 35 with four of 128 threads and 8 queries each).  A thread owns 4 queries x 4 keys of a tile's logits and 4 queries x d / 16 elements of the
+// window 256: 46 us with one group, 30.8 with two, 35 with four of 128 threads and 8 queries each).  A thread owns 4 queries x 4 keys of a tile's logits and 4 queries x d / 16 elements of the
 // output (packed FMAs); keys come through registers (transposed), values by asynchronous copies beside the logits, the weights go
-// through shared memory.  Everything in fp32.  Bound by the latency of shared memory and the FMA pipe: two loads of 16 bytes feed 16
-// FMAs per thread.
+// through shared memory.  Everything in fp32.  Bound by shared memory (L1 81 % busy, FMA 25 % of its issue): two loads of 16 bytes feed 16
+// FMAs per thread.  8 heads of 2000 tokens: d = 64 145 us, d = 128 259 (28 and 32 TFLOP/s).
 #include <math.h>
 
 #include <algorithm>

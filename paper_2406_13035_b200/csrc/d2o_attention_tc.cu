@@ -15,11 +15,13 @@
 // commit that announces a new S covers every product issued ahead of it.
 //
 // What bounds it: neither the tensor cores (57 % busy) nor the exponentials (57 %) but a query tile's chain from S to the next S, 3000 - 3200
-// cycles against 2050 of products for both tiles; under load the power cap.  us: 32 / 8 heads of 32768 tokens under a window of 4096, bf16, 1800 cool and
-// 2190 warm (1.15 and 0.94 PFLOP/s); four ragged prompts of up to 6001 tokens 450 - 505; 32 heads of 1200 tokens 28.
+// cycles against 2050 of products for both tiles; under load the power cap.  us: 32 / 8 heads of 32768 tokens under a window of 4096, bf16, 1860 cool and
+// 2150 warm (1.11 and 0.96 PFLOP/s); four ragged prompts of up to 6001 tokens 340 - 620 (0.93 - 1.06 PFLOP/s); 32 heads of 1200 tokens 27 - 28; 32 / 8 heads of
+// 8192 tokens, d = 64, 389 (0.71).
 //
 // Rounding: weights to the input type for their product (relative half step 2^-8 bf16, 2^-11 fp16; the errors of many keys average out.
-// fp16 weights below 2^-21 of the row's largest are subnormal: off by up to 2^-32 of that, the most keys, 2^20, together by 2^-12); their sum and lse from the unrounded ones; S, O and all sums are fp32.
+// fp16 weights below 2^-21 of the row's largest are subnormal: off by up to 2^-32 of that, the most keys, 2^20, together by 2^-12);
+// their sum and lse from the unrounded ones; S, O and all sums are fp32.
 #include <math.h>
 
 #include <cuda/std/type_traits>

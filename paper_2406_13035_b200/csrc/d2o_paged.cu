@@ -138,7 +138,7 @@ struct EvictExchange {                       // read by the other CTAs of the cl
 // sources and targets do not overlap, so that all moves run at once.  (4) The moves, divided over the cluster, several rows of a
 // group of lanes in flight.  What costs are the dependent steps.  us, counting lane by lane, numbering by block scans twice, one row in
 // flight, clusters of at most eight / so (with the copy that restores the scores): 8 slices of 32768 rows to 6554 63 / 34 (selection 15, moves
-// 9 at 5 TB/s), 256 slices of 2064 rows to 2048 31 / 16.
+// 9 at 5 TB/s), 256 slices of 2064 rows to 2048 31 / 16.  Stalls: loads, then the barriers; DRAM 9 % busy.
 template <int ROWB, bool CL>
 __global__ void __launch_bounds__(kEvictThreads, 2)
 evict_kernel(EvictArgs a) {
@@ -410,8 +410,9 @@ cudaError_t launch_paged_evict(const PagedView& p, int dtype, int D, const int32
   const PagedScratch s(n_slices, p.Hq / p.Hkv, D, (size_t)p.n_pages * p.Hkv << p.page_shift, true);
   const EvictArgs a = {p, budgets, next_pos, reinterpret_cast<int2*>(scratch + s.rows), n_sink, window};
   // One CTA per SM, as long as the table could hold 1024 rows for each of a cluster (the rows are known on the device only).  us with the
-  // restoring copy, 8 slices: of 100 rows 7.2 (one CTA) against 15.7 (sixteen), of 1100 10.4 / 16.4, of 5300 18.4 (four) against 29.0 (one)
-  // and 19.3 (sixteen), of 9000 19.6 (eight) / 32.9 / 22.0.
+  // restoring copy, 8 slices: of 100 rows to 50 7.2 (one CTA) against 15.7 (sixteen), of 1100 to 1000 10.4 / 16.4, of 5300 to 4300 18.4 (four)
+  // against 29.0 (one) and 19.3 (sixteen), of 9000 to 2000 19.6 (eight) / 32.9 / 22.0.  So few rows in a table with room for many pay for the
+  // cluster that they do not need.
   int C = 1;
   const long long reach = (long long)p.max_pages << p.page_shift;
   while (2 * C <= kEvictMaxCluster && (long)n_slices * 2 * C <= sms && reach >= (long long)kEvictMinRows * 2 * C) C *= 2;

@@ -9,9 +9,10 @@
 // the logits go to scratch on the way, and score_kernel, which knows the normalisers, adds the weights to the rows' scores.
 //
 // Bound by HBM where there is enough to read, by a chain of dependent steps elsewhere (lengths, page numbers, rows, softmax, join).
-// us on the GPU: one sequence of 131072 rows (8 KV heads of four query heads, bf16, d = 128: 537 MB) 91 (5.9 TB/s; the slowest SMs take 15 %
-// longer than the mean); 32 sequences of up to 16384 rows under a window of 2048 (270 MB) 54; 8 of up to 4096 rows, 32 heads, with scores (255 MB) 51;
-// one of 1640 rows 8.5; 25 of up to 8 rows 9.6.
+// us: one sequence of 131072 rows (8 KV heads of four query heads, bf16, d = 128: 537 MB) 89 - 94 (5.7 - 6.0 TB/s; the slowest SMs take 15 %
+// longer than the mean), heads of one or two 87, of eight 95; d = 64 with heads of one 49 (5.5 TB/s), four 52, eight 69 (3.9); fp32 211 (5.1), d = 64
+// 99 (5.4); 32 sequences of up to 16384 rows under a window of 2048 (270 MB) 54; 8 of up to 4096 rows, 32 heads, with scores (255 MB) 54; in a graph
+// one of 1640 rows 8.6, 25 of up to 8 rows 9.0.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -886,7 +887,8 @@ score_kernel(PagedDecodeArgs a) {
 // (the portable size; for up to three quarters of the SMs, because sixteen clusters of eight are not resident at once), as long as what
 // the table can hold gives a CTA at most 64 tiles (16-bit rows of d = 128: 512 KB, 10 us).  us, shares / clusters, 8 KV heads, d = 128, bf16: one
 // sequence of 3000 rows 11.7 / 9.0, of 7000 17.0 / 12.6, two of 3000 15.1 / 11.1 (16.9 with eight CTAs each), four of 3000 16.8 / 11.6; nine
-// ragged ones of up to 3500 (beyond the bound) 16.5 / 18.2.
+// ragged ones of up to 3500 (beyond the bound) 16.5 / 18.2.  The lengths are not known here: one sequence in a table with room for sixteen times its
+// rows gets shares, and their times.
 static int paged_cluster(const PagedView& p, int n_slices, int sms) {
   int C = 1;
   while (2 * C <= 1 << (kPagedClusters - 1) && (long)n_slices * 2 * C <= (2 * C < 8 ? sms : sms * 3 / 4)) C *= 2;
