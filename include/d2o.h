@@ -416,8 +416,8 @@ d2o_status d2o_set_fault_injection(d2o_ctx* ctx, int32_t wait_limit_us, int32_t 
 /* The same for the 16-bit kernels of d2o_prompt_attention and d2o_paged_decode_step, which have no context: for the whole process, from the next
  * call on (a call captured into a graph keeps what held when it was captured).  producer_stop_stage: the prompt attention copies no tile of
  * keys or values from this one of every thread block on, the decode step does not copy the tile of this number (-1 = never).
- * late_answers = 1: the answers by which thread blocks of the prompt attention take over the work of others count as late.  (0, -1, 0) is
- * the ordinary state. */
+ * late_answers > 0: the answers by which a thread block of the prompt attention takes over the work of others count as late, from
+ * this one on.  (0, -1, 0) is the ordinary state. */
 d2o_status d2o_set_static_fault_injection(int32_t wait_limit_us, int32_t producer_stop_stage, int32_t late_answers);
 
 #ifdef __cplusplus

@@ -444,9 +444,9 @@ def d2o_prompt_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, out:
           _arg(status, "status", (2,), torch.int32, dev))
 
 
-def d2o_set_static_fault_injection(wait_limit_us: int = 0, producer_stop_stage: int = -1, late_answers: bool = False):
+def d2o_set_static_fault_injection(wait_limit_us: int = 0, producer_stop_stage: int = -1, late_answers: int = 0):
     """For failure-detection tests of the calls without a context; the defaults are the ordinary state."""
-    _check(load_library().d2o_set_static_fault_injection(wait_limit_us, producer_stop_stage, int(late_answers)), "d2o_set_static_fault_injection")
+    _check(load_library().d2o_set_static_fault_injection(wait_limit_us, producer_stop_stage, late_answers), "d2o_set_static_fault_injection")
 
 
 class D2OPagedCache:

@@ -14,7 +14,7 @@ struct PromptAttentionArgs {
   int B, Hq, Hkv, P, window, n_sink;         // window: P where there is none
   unsigned long long wait_ns;                // limit of every wait (16-bit kernel)
   int stop_stage;                            // failure-detection tests: no copy of keys or values from this one of a CTA on; -1: never
-  int late_answers;                          // failure-detection tests: answers to requests for work count as late
+  int late_answers;                          // failure-detection tests: a CTA's answers to requests for work count as late from this one on; 0: none
 
   __device__ __forceinline__ int length(int b) const { return lens ? max(0, min(lens[b], P)) : P; }
   // does query i see key j (of a sequence that has both)?

@@ -172,13 +172,15 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   unsigned char* sKV = pa_smem + 2 * TILE;                   // [stages][KB][128 rows][128 B]
   __shared__ unsigned long long q_full, q_empty, kv_full[STAGES], kv_empty[STAGES], s_full[2], p_ready[2][2], o_full[2], o_empty[2], turn[2], all_done[2], it_full[2], it_empty[2], answered;
   __shared__ alignas(16) uint4 s_answer;
-  __shared__ volatile int s_item[2], s_lost;                 // this CTA's current and next item; given to it after a wait had run out; -1: none
+  // This CTA's items: the one that the slowest warp has taken, the next, and the one that is announced while that warp is at the first; the
+  // item that it was given after a wait had run out.  -1: none.
+  __shared__ volatile int s_item[3], s_lost;
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_fail;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
-    s_item[0] = s_item[1] = s_lost = -1;
+    s_item[0] = s_item[1] = s_item[2] = s_lost = -1;
     s_fail = (tc::smem_u32(pa_smem) & 1023u) != 0u;          // swizzled tiles need 1024-byte aligned shared memory
     tc::mbar_init(&q_full, 1); tc::mbar_init(&q_empty, 2); tc::mbar_init(&answered, 1);
     for (int s = 0; s < STAGES; ++s) { tc::mbar_init(&kv_full[s], 1); tc::mbar_init(&kv_empty[s], 2); }
@@ -206,7 +208,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
   // The k-th item of this CTA as a warp sees it; -1: no more.
   auto next_item = [&](int k) {
     if (!__all_sync(0xffffffffu, wait(&it_full[k & 1], (uint32_t)((k >> 1) & 1)))) return -1;
-    const int i = s_item[k & 1];
+    const int i = s_item[k % 3];
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(&it_empty[k & 1]);
     return i;
@@ -222,7 +224,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       for (int k = 0;; ++k) {
         if (k >= 2) (void)wait(&it_empty[k & 1], (uint32_t)(((k >> 1) - 1) & 1));
         if (s_fail) { s_lost = i; break; }                   // the others run out of time, too
-        s_item[k & 1] = i;
+        s_item[k % 3] = i;
         tc::mbar_arrive(&it_full[k & 1]);
         if (i < 0) break;
         const PaItem it(a, i);
@@ -247,7 +249,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         // Not earlier: the loads are two tiles of keys ahead of the products, which covers the answer's way, and an item asked for at the
         // beginning of a long one would wait while other CTAs have nothing to do (1200 tokens of 32 heads: 36 us instead of 30).
         tc::ask_for_cta(&s_answer, &answered);
-        if (!a.late_answers && wait(&answered, (uint32_t)(k & 1))) {
+        if ((a.late_answers == 0 || k + 1 < a.late_answers) && wait(&answered, (uint32_t)(k & 1))) {
           i = tc::cta_answered(&s_answer);
         } else {                                             // the CTA that it may name will not start: looked at again below
           s_fail = 1; unanswered = k; i = -1;
@@ -458,8 +460,8 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       if (a.status) report_error(a.status, D2O_ERR_TIMEOUT, 0xA7710000u | (uint32_t)(blockIdx.x & 0xffff));
     }
     __syncthreads();
-    for (int x = 0; x < 3; ++x) {                            // NaN for the items in hand
-      const int i = x < 2 ? s_item[x] : s_lost;
+    for (int x = 0; x < 4; ++x) {                            // NaN for the items in hand
+      const int i = x < 3 ? s_item[x] : s_lost;
       if (i < 0) continue;
       const PaItem it(a, i);
       for (int r = it.q0 + tid; r < min(it.P, it.q0 + 2 * kPaTile); r += kPaThreads) {

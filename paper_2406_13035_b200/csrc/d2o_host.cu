@@ -589,7 +589,7 @@ extern "C" d2o_status d2o_full_decode_step(int32_t dtype, int32_t d_head, int32_
 static std::atomic<int> g_wait_limit_us{0}, g_stop_stage{-1}, g_late_answers{0};
 
 extern "C" d2o_status d2o_set_static_fault_injection(int32_t wait_limit_us, int32_t producer_stop_stage, int32_t late_answers) {
-  if (wait_limit_us < 0 || producer_stop_stage < -1 || late_answers < 0 || late_answers > 1) return D2O_ERR_INVALID_ARG;
+  if (wait_limit_us < 0 || producer_stop_stage < -1 || late_answers < 0) return D2O_ERR_INVALID_ARG;
   g_wait_limit_us = wait_limit_us;
   g_stop_stage = producer_stop_stage;
   g_late_answers = late_answers;

@@ -42,7 +42,7 @@ def test_prompt_attention_answers_that_come_late(cuda_device, knob, dtype, d, b,
     B.d2o_prompt_attention(q, k, v, want, lens=dl)
     out, lse = torch.full_like(q, 7.0), torch.full((b, hq, n), 7.0, device="cuda")
     status = torch.zeros(2, dtype=torch.int32, device="cuda")
-    knob(2000, -1, True)
+    knob(2000, -1, 1)
     _timed(lambda: B.d2o_prompt_attention(q, k, v, out, lse=lse, lens=dl, status=status))
     assert status.tolist()[0] == D2O_ERR_TIMEOUT
     for i, m in enumerate(lens):
@@ -52,6 +52,23 @@ def test_prompt_attention_answers_that_come_late(cuda_device, knob, dtype, d, b,
     status.zero_()
     B.d2o_prompt_attention(q, k, v, out.fill_(7.0), lens=dl, status=status)
     assert torch.equal(out, want) and status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("b,hq,hkv,n", [(40, 64, 8, 100), (10, 64, 8, 300), (2, 40, 8, 1500)])
+def test_prompt_attention_answers_that_come_late_later_on(cuda_device, knob, dtype, d, b, hq, hkv, n):
+    """Blocks that go on for a while, and lose an answer while up to two items ahead of the one that it was asked behind are in work: every row is right or
+    NaN, none keeps what it held."""
+    q, k, v = _prompt(dtype, d, b, hq, hkv, n)
+    want = torch.empty_like(q)
+    B.d2o_prompt_attention(q, k, v, want)
+    status = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for late in (2, 3, 4, 5) * 6:
+        out, lse = torch.full_like(q, 7.0), torch.full((b, hq, n), 7.0, device="cuda")
+        knob(2000, -1, late)
+        _timed(lambda: B.d2o_prompt_attention(q, k, v, out, lse=lse, status=status))
+        bad = out.isnan().all(-1)
+        assert bool((bad | (out == want).all(-1)).all()) and torch.equal(bad, lse.isnan()), int((~bad & (out == 7.0).all(-1)).sum())
 
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64)])
