@@ -202,12 +202,15 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
     s_fail = 1;
     return false;
   };
+  // Of a warp that walks together: its threads may run out of time apart, and those that stayed would wait for the others, at the next
+  // instruction of the whole warp, for good.
+  auto wait_warp = [&](unsigned long long* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
   start_dependents();
   wait_for_prior_grid();
   int loads_q = 0, loads_kv = 0, unanswered = -1;            // of the producer; the request whose answer was not there in time
   // The k-th item of this CTA as a warp sees it; -1: no more.
   auto next_item = [&](int k) {
-    if (!__all_sync(0xffffffffu, wait(&it_full[k & 1], (uint32_t)((k >> 1) & 1)))) return -1;
+    if (!wait_warp(&it_full[k & 1], (uint32_t)((k >> 1) & 1)) || __any_sync(0xffffffffu, s_fail != 0)) return -1;
     const int i = s_item[k % 3];
     __syncwarp();
     if (lane == 0) tc::mbar_arrive(&it_empty[k & 1]);
@@ -263,8 +266,8 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
     const int t = warp - kPaSoftWarps - 1;
     const uint32_t ts = tm_s + t * 128, to = tm_o + t * 128;
     int ring = 0, items = 0, turns = 0, np = 0, no = 0;      // tiles of keys or values, items, turns, weights taken, outputs begun
-    auto full = [&](int slot) { return wait(&kv_full[slot % STAGES], (uint32_t)((slot / STAGES) & 1)); };
-    for (int x = 0, i; (i = next_item(x)) >= 0 && !s_fail; ++x) {
+    auto full = [&](int slot) { return wait_warp(&kv_full[slot % STAGES], (uint32_t)((slot / STAGES) & 1)); };
+    for (int x = 0, i; (i = next_item(x)) >= 0; ++x) {
       const PaItem it(a, i);
       if (it.empty()) continue;
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
@@ -277,7 +280,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         tc::mma_commit_one(&s_full[t]);
       };
       uint32_t begun = 0;
-      if (!wait(&q_full, (uint32_t)(items & 1)) || !full(ring)) break;
+      if (!wait_warp(&q_full, (uint32_t)(items & 1)) || !full(ring)) break;
       ++items;
       tc::fence_after_sync();
       bool now = pa_valid(a, w0, it.P, span.tile(0) * kPaTile);      // does the tile see anything of job j?
@@ -302,13 +305,13 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
           __syncwarp();
         }
         if (j + 1 < n && !full(ring + 1)) break;
-        if (now && !begun && no++ > 0 && !wait(&o_empty[t], (uint32_t)(no & 1))) break;
-        if (!wait(&turn[t], (uint32_t)((turns++ & 1) ^ (t ^ 1)))) break;
+        if (now && !begun && no++ > 0 && !wait_warp(&o_empty[t], (uint32_t)(no & 1))) break;
+        if (!wait_warp(&turn[t], (uint32_t)((turns++ & 1) ^ (t ^ 1)))) break;
         if (now) {
           const uint64_t bd = tc::smem_desc_sw128_mn(tc::smem_u32(sKV + ring % STAGES * TILE), BLOCK);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {                      // the weights of 64 keys at a time
-            (void)wait(&p_ready[t][h], (uint32_t)(np & 1));
+            (void)wait_warp(&p_ready[t][h], (uint32_t)(np & 1));
             tc::fence_after_sync();
 #pragma unroll
             for (int k = h * kPaTile / 32; k < (h + 1) * kPaTile / 32; ++k)      // 16 keys: 8 columns of weights, 16 rows of 128 bytes of V
@@ -329,10 +332,9 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         now = next;
       }
     }
-    if (s_fail && lane == 0) {                               // tensor memory is freed behind the last products
-      tc::mma_commit(&all_done[t]);
-      (void)tc::mbar_wait(&all_done[t], 0);
-    }
+    // Tensor memory is freed behind the last products, also where the softmax warps run out of time after this one has left the loop.
+    tc::mma_commit_one(&all_done[t]);
+    if (lane == 0) (void)tc::mbar_wait(&all_done[t], 0);
     __syncwarp();
   }
   } else {
@@ -342,7 +344,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t ts = tm_s + t * 128 + lanes, to = tm_o + t * 128 + lanes;
     int ns = 0, items = 0;
-    for (int x = 0, i; (i = next_item(x)) >= 0 && !s_fail; ++x) {
+    for (int x = 0, i; (i = next_item(x)) >= 0; ++x) {
       const PaItem it(a, i);
       if (it.empty() || !it.exists(t)) continue;
       const PromptSpan span(it.q0, 2 * kPaTile, it.P, kPaTile, a.window, a.n_sink);
@@ -351,7 +353,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
       for (int j = 0; j < span.tiles; ++j) {
         const int k0 = span.tile(j) * kPaTile;
         if (!pa_valid(a, w0, it.P, k0)) continue;
-        if (!__all_sync(0xffffffffu, wait(&s_full[t], (uint32_t)(ns++ & 1)))) break;
+        if (!wait_warp(&s_full[t], (uint32_t)(ns++ & 1))) break;
         tc::fence_after_sync();
         uint32_t s0[32], s1[32], s2[32], s3[32];
         tc::tmem_ld32_issue(ts, s0); tc::tmem_ld32_issue(ts + 32, s1);
@@ -414,7 +416,7 @@ prompt_attention_tc_kernel(PromptAttentionArgs a, const __grid_constant__ PaMaps
         tc::unpack2(tc::add2(sum[0], sum[1]), lo, hi);
         l += lo + hi;
       }
-      if (!__all_sync(0xffffffffu, wait(&o_full[t], (uint32_t)(items++ & 1)))) break;
+      if (!wait_warp(&o_full[t], (uint32_t)(items++ & 1))) break;
       tc::fence_after_sync();
       const float f = 1.f / l;
       T* out = (T*)a.out + ((size_t)it.bh * a.P + row) * D;

@@ -140,3 +140,28 @@ def test_decode_step_whose_tiles_do_not_arrive(cuda_device, knob, dtype, d, G, b
     c.check()
     zero = c._scratch[0] - c.scratch.data_ptr()
     assert not c.scratch[zero:zero + B.PAGED_ZERO_BYTES].any()
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f16", 64), ("f16", 128), ("bf16", 64)])
+@pytest.mark.parametrize("b,hq,hkv,n", [(40, 64, 8, 100), (10, 64, 8, 300), (2, 40, 8, 1500), (1, 8, 8, 3000)])
+def test_prompt_attention_with_hardly_any_patience(cuda_device, knob, dtype, d, b, hq, hkv, n):
+    """Limits of a few microseconds, so that any wait runs out in any state of a block: every row is right or NaN, none keeps what it held; and the error
+    word says so."""
+    q, k, v = _prompt(dtype, d, b, hq, hkv, n)
+    want = torch.empty_like(q)
+    B.d2o_prompt_attention(q, k, v, want)
+    failed = 0
+    for limit in (1, 1, 1, 2, 2, 3, 3, 4, 5, 6, 8, 11, 15, 20):
+        out, lse = torch.full_like(q, 7.0), torch.full((b, hq, n), 7.0, device="cuda")
+        status = torch.zeros(2, dtype=torch.int32, device="cuda")
+        knob(limit)
+        _timed(lambda: B.d2o_prompt_attention(q, k, v, out, lse=lse, status=status))
+        bad = out.isnan().all(-1)
+        assert bool((bad | (out == want).all(-1)).all()) and torch.equal(bad, lse.isnan()), (limit, int((~bad & (out != want).any(-1)).sum()))
+        assert status.tolist()[0] == D2O_ERR_TIMEOUT or not bool(bad.any())
+        failed += bool(bad.any())
+    assert failed
+    knob()
+    out = torch.empty_like(q)
+    B.d2o_prompt_attention(q, k, v, out)
+    assert torch.equal(out, want)
