@@ -647,7 +647,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
     const int r = x.row0(), row0 = p.page_row0(x.b, x.h, r);
     return row0 < 0 ? -1 : row0 + p.in_page(r);
   };
-  int asked = 0, ask_row = -1;
+  int asked = 0, ask_row = -1, missing = -1;                 // lane 0: the copy that a test left out
   unsigned long long drop;                                   // read once
   asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(drop));
   auto copy = [&](long long at, int row) {                   // of the tile at pool row `row`
@@ -657,6 +657,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
       s_row[warp][s] = row;
       unsigned char* to = my_ring + s * 2 * TILE;
       if (a.stop_stage >= 0 && at - first == a.stop_stage) {             // never arrives
+        missing = asked;
       } else if (row >= 0) {
         tc::mbar_expect_tx(&s_full[warp][s], 2 * TILE);
 #pragma unroll
@@ -723,7 +724,7 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
       const int row0 = span.row0((int)(mine - cur.before)), prow = s_row[warp][s];
       unsigned char* stage = my_ring + s * 2 * TILE;
       if (prow < 0 || lost) {
-        if (lane == 0 && prow < 0) p.report(kPagedBadPage);
+        if (lane == 0 && !lost) p.report(kPagedBadPage);
         l[0] = l[1] = NAN;
         __syncwarp();
         if (!lost) request();
@@ -838,7 +839,8 @@ paged_decode_tc_kernel(PagedDecodeArgs a, const __grid_constant__ PagedMaps maps
   if (__syncthreads_or(lost)) {                              // the last parts are combined
     if (tid == 0 && p.status) report_error(p.status, D2O_ERR_TIMEOUT, 0x9A6E3000u);
     // see the copies on their way land before the CTA may end, and before a cluster's part, which lies in the ring's place, is read
-    for (int i = max(0, asked - STAGES); i < asked; ++i) (void)tc::mbar_wait(&s_full[warp][i % STAGES], (uint32_t)((i / STAGES) & 1), a.wait_ns);
+    for (int i = max(0, asked - STAGES); lane == 0 && i < asked; ++i)
+      if (i != missing) (void)tc::mbar_wait(&s_full[warp][i % STAGES], (uint32_t)((i / STAGES) & 1));
     __syncthreads();
     if (CL && tid < G) reinterpret_cast<float*>(paged_smem)[tid * (D + 4) + D + 1] = NAN;
   }

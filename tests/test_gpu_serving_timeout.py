@@ -165,3 +165,43 @@ def test_prompt_attention_with_hardly_any_patience(cuda_device, knob, dtype, d, 
     out = torch.empty_like(q)
     B.d2o_prompt_attention(q, k, v, out)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("dtype,d,G", [("bf16", 128, 4), ("f16", 64, 1), ("bf16", 64, 8), ("f16", 128, 2)])
+@pytest.mark.parametrize("b,held,room", [(1, 900, 1000), (3, 2500, 20000), (60, 200, 400), (16, 3000, 6000)])
+def test_decode_step_with_hardly_any_patience(cuda_device, knob, dtype, d, G, b, held, room):
+    """The same for the decode step: every slice's outputs are right or NaN."""
+    page, hkv = 16, 8
+    g = torch.Generator(device="cuda").manual_seed(held + d)
+    used = held // page + 1
+    table = torch.full((b, room // page), -1, dtype=torch.int32, device="cuda")
+    table[:, :used] = torch.randperm(b * used, generator=g, device="cuda").view(b, used).to(torch.int32)
+    kp, vp = (torch.randn(b * used, hkv, page, d, generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    length = torch.randint(0, held + 1, (b, hkv), generator=g, device="cuda", dtype=torch.int32)
+    q, k, v = (torch.randn(b, h, d, generator=g, device="cuda").to(DT[dtype]) for h in (hkv * G, hkv, hkv))
+    c = B.D2OPagedCache(kp, vp, table, length, n_q_heads=hkv * G)
+    want = torch.empty_like(q)
+    c.d2o_paged_decode_step(q, k, v, want)
+    c.check()
+    for limit in (1, 1, 1, 2, 2, 3, 4, 5, 6, 8, 11):
+        flush = torch.zeros(1 << 28, dtype=torch.uint8, device="cuda")          # the rows come from memory
+        out = torch.full_like(q, 7.0)
+        knob(limit)
+        _timed(lambda: c.d2o_paged_decode_step(q, k, v, out))
+        bad = out.view(b * hkv, G * d).isnan()
+        assert bool((bad.all(-1) == bad.any(-1)).all())
+        right = (out.view(b * hkv, G * d) == want.view(b * hkv, G * d)).all(-1)
+        assert bool((bad.all(-1) | right).all()), limit
+        if bool(bad.any()):
+            with pytest.raises(B.D2OError) as e:
+                c.check()
+            assert e.value.status == D2O_ERR_TIMEOUT
+        c.status.zero_()
+        del flush
+    knob()
+    out = torch.empty_like(q)
+    c.d2o_paged_decode_step(q, k, v, out)
+    assert torch.equal(out, want)
+    c.check()
+    zero = c._scratch[0] - c.scratch.data_ptr()
+    assert not c.scratch[zero:zero + B.PAGED_ZERO_BYTES].any()
