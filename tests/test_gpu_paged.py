@@ -392,6 +392,47 @@ def test_decode_offsets_past_32_bits(cuda_device):
     c.check()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_and_eviction_past_32_bits(cuda_device, dtype):
+    """The same with scores: a step and an eviction in pages behind the border, which move nothing and touch no score elsewhere."""
+    page, d, hkv, G, dt = 1024, 128, 4, 2, DT[dtype]
+    n_pages = (1 << 31) // (page * d * hkv) + 8
+    kp = torch.zeros(n_pages, hkv, page, d, dtype=dt, device="cuda")
+    vp = torch.zeros_like(kp)
+    pos, score = torch.zeros(n_pages, hkv, page, dtype=torch.int32, device="cuda"), torch.zeros(n_pages, hkv, page, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    table = torch.tensor([[n_pages - 1, 1, n_pages - 4]], dtype=torch.int32, device="cuda")
+    n, keep = 2 * page + 77, 900
+    for i, p in enumerate(table[0].tolist()):
+        kp[p], vp[p] = (torch.randn(hkv, page, d, generator=g, device="cuda").to(dt) for _ in range(2))
+        pos[p] = torch.arange(i * page, (i + 1) * page, device="cuda", dtype=torch.int32)
+    length = torch.full((1, hkv), n, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(1, h, d, generator=g, device="cuda").to(dt) for h in (hkv * G, hkv, hkv))
+    out = torch.empty_like(q)
+    c = B.D2OPagedCache(kp, vp, table, length, n_q_heads=hkv * G, pos=pos, score=score)
+    c.d2o_paged_decode_step(q, k, v, out)
+    dense = lambda pool: pool[table[0].long()].transpose(0, 1).flatten(1, 2)[:, :n + 1]
+    K, V = dense(kp).double(), dense(vp).double()
+    assert torch.equal(K[:, n], k[0].double()) and torch.equal(V[:, n], v[0].double())
+    p = torch.softmax(torch.einsum("hgd,hnd->hgn", q[0].double().view(hkv, G, d), K) / math.sqrt(d), -1)
+    torch.testing.assert_close(out[0].double().view(hkv, G, d), p @ V, rtol=2.0 ** -8, atol=1e-5)
+    torch.testing.assert_close(dense(score).double(), p.sum(1), rtol=1e-4, atol=1e-9)
+    assert int((score != 0).sum()) == hkv * (n + 1)
+    length += 1
+    was_k, was_v, was_s, was_p = (dense(t).clone() for t in (kp, vp, score, pos))
+    c.d2o_paged_evict(torch.full((1, hkv), keep, dtype=torch.int32, device="cuda"), torch.tensor([n + 1], dtype=torch.int32, device="cuda"), n_sink=2, window=50)
+    rank = was_s.double() + ((was_p < 2) | (was_p >= n + 1 - 50)) * 1e9 - was_p.double() * 1e-18
+    for h in range(hkv):
+        stays = torch.zeros(n + 1, dtype=torch.bool, device="cuda")
+        stays[rank[h].topk(keep).indices] = True
+        to, frm = (~stays[:keep]).nonzero()[:, 0], stays[keep:].nonzero()[:, 0] + keep
+        src = torch.arange(keep, device="cuda")
+        src[to] = frm
+        for pool, was in ((kp, was_k), (vp, was_v), (score, was_s), (pos, was_p)):
+            assert torch.equal(dense(pool)[h, :keep], was[h, src]) and torch.equal(dense(pool)[h, keep:], was[h, keep:])
+    c.check()
+
+
 # ---------------------------------------------------------------------------------------------- many, at once, and with one scratch
 def _batch(seed, b, hkv, G, d, dtype, page, held, scored=False):
     """A cache made on the GPU, lengths 0 .. held; returns it with its tensors and a function for the float64 output of one slice."""

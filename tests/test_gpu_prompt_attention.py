@@ -269,6 +269,36 @@ def test_normalisers_feed_the_column_sums(cuda_device):
     torch.testing.assert_close(sums[0], sums[1], rtol=2e-5, atol=1e-7)
 
 
+@pytest.mark.parametrize("dtype,d,hq", [("bf16", 128, 17), ("f16", 64, 34), ("f32", 128, 17)])
+def test_longest_prompt_and_offsets_past_32_bits(cuda_device, dtype, d, hq):
+    """2^20 tokens under a window, more than 2^31 elements of queries: rows of the first and of the last head."""
+    n, window, sinks = 1 << 20, 300, 5
+    g = torch.Generator(device="cuda").manual_seed(hq)
+    q, k, v = (torch.empty(1, h, n, d, dtype=DT[dtype], device="cuda").normal_(generator=g) for h in (hq, 1, 1))
+    out, lse = torch.full_like(q, float("nan")), torch.full((1, hq, n), float("nan"), device="cuda")
+    status = torch.zeros(2, dtype=torch.int32, device="cuda")
+    B.d2o_prompt_attention(q, k, v, out, lse=lse, window=window, n_sink=sinks, status=status)
+    assert status.tolist() == [0, 0]
+    for h in (0, hq - 1):
+        for end in (600, n // 2 + 77, n):
+            a = end - 600
+            cols = torch.cat([torch.arange(min(sinks, max(0, a - window)), device="cuda"), torch.arange(max(0, a - window), end, device="cuda")])
+            K, V = k[0, 0, cols], v[0, 0, cols]
+            rows = torch.arange(a, end, device="cuda")
+            i, j = rows[:, None], cols[None]
+            seen = (j <= i) & ((j > i - window) | (j < sinks))
+            Q = q[0, h, rows].double()
+            x = (Q @ K.double().T / math.sqrt(d)).masked_fill(~seen, -math.inf)
+            y = torch.logsumexp(x, 1)
+            p = torch.exp(x - y[:, None])
+            delta = 16 * 2.0 ** -24 * float((Q.abs() @ K.double().abs().T).max()) / math.sqrt(d)
+            weights = 0.0 if dtype == "f32" else torch.finfo(DT[dtype]).eps / 2
+            e, ref, o = (weights + 2 * delta + 2.0 ** -21) * (p @ V.double().abs()), p @ V.double(), out[0, h, rows].double()
+            assert bool((((ref - e).to(DT[dtype]).double() <= o) & (o <= (ref + e).to(DT[dtype]).double())).all()), (h, end)
+            assert bool(((lse[0, h, rows].double() - y).abs() <= delta + 2.0 ** -22 * y.abs().clamp(min=1)).all())
+    assert not bool(lse.isnan().any()) and not any(bool(out[0, h].isnan().any()) for h in range(hq))
+
+
 def test_streams_graph_and_repeats(cuda_device):
     """On a stream other than the default one, captured and replayed with other inputs, the same bits every time."""
     q, k, v = draw(11, 2, 4, 2, 385, 128, "f16")
